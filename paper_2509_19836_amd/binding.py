@@ -1,4 +1,4 @@
-"""ctypes binding of libburstattn's C ABI (include/burst_attn.h).
+"""ctypes binding of libburstattn's C ABI (include/burst_attn.h, burst_lm_head.h and burst_attn_cache.h).
 
 Argument marshalling only: every function here has the name of the C entry point
 it calls and does nothing but describe torch tensors as (pointer, strides) and
@@ -21,7 +21,7 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 BURST_OK, BURST_ERR_INVALID_ARG, BURST_ERR_UNSUPPORTED, BURST_ERR_HIP, BURST_ERR_SCRATCH = 0, -1, -2, -3, -4
-BURST_BF16, BURST_F32 = 0, 1
+BURST_BF16, BURST_F32, BURST_F8E4M3 = 0, 1, 2
 BURST_MASK_FULL, BURST_MASK_CAUSAL = 0, 1
 BURST_ACC_DQ, BURST_ACC_DK, BURST_ACC_DV = 1, 2, 4
 BURST_MAX_STEPS = 1024
@@ -116,6 +116,30 @@ _lib.burst_lm_head_loss_noalloc.restype = C.c_int
 _lib.burst_lm_head_loss_noalloc.argtypes = [_P(burst_lm_head_shape_t), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
                                             C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int64,
                                             C.c_int32, C.c_void_p]
+
+
+class burst_rope_t(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("rotary_dim", C.c_int32), ("adjacent", C.c_int32), ("_pad", C.c_int32),
+                ("inv_freq", C.c_void_p), ("positions", C.c_void_p), ("stride_axis", C.c_int64), ("stride_b", C.c_int64),
+                ("axis_of_pair", C.c_uint8 * 64)]
+
+
+class burst_cache_t(C.Structure):
+    _fields_ = [("k", burst_tensor_t), ("v", burst_tensor_t), ("n_pages", C.c_int64), ("page_rows", C.c_int32),
+                ("table_cols", C.c_int32), ("table", C.c_void_p), ("table_stride", C.c_int64), ("rows", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+_lib.burst_attn_rope.restype = C.c_int
+_lib.burst_attn_rope.argtypes = [_P(burst_shape_t), _P(burst_rope_t)] + [_P(burst_tensor_t)] * 4 + [C.c_int32, C.c_void_p]
+_lib.burst_attn_cache_append.restype = C.c_int
+_lib.burst_attn_cache_append.argtypes = [_P(burst_shape_t), _P(burst_cache_t), _P(burst_tensor_t), _P(burst_tensor_t), C.c_void_p,
+                                         _P(burst_rope_t), _P(burst_tensor_t), _P(burst_tensor_t), C.c_void_p]
+_lib.burst_attn_decode_workspace_bytes.restype = C.c_int64
+_lib.burst_attn_decode_workspace_bytes.argtypes = [_P(burst_shape_t)]
+_lib.burst_attn_decode.restype = C.c_int
+_lib.burst_attn_decode.argtypes = [_P(burst_shape_t), _P(burst_cache_t), _P(burst_tensor_t), C.c_void_p, _P(burst_tensor_t),
+                                   _P(burst_rowvec_t), C.c_void_p, C.c_int64, C.c_void_p]
 _lib.burst_attn_status_string.restype = C.c_char_p
 _lib.burst_attn_status_string.argtypes = [C.c_int]
 _lib.burst_attn_last_hip_error.restype = C.c_int
@@ -127,7 +151,8 @@ EXPORTS = ["burst_attn_step_fwd", "burst_attn_steps_fwd", "burst_attn_steps_bwd"
            "burst_attn_fill_block_striped_mask",
            "burst_attn_visible_pairs", "burst_attn_tile_class", "burst_attn_visible_tile_runs", "burst_attn_visible_rows", "burst_attn_mfma_probe", "burst_attn_set_chunk_rows", "burst_attn_chunk_plan", "burst_attn_launch_plan", "burst_attn_status_string", "burst_attn_last_hip_error",
            "burst_attn_version", "burst_lm_head_workspace_bytes", "burst_lm_head_loss",
-           "burst_lm_head_static_scratch_bytes", "burst_lm_head_tile_plan", "burst_lm_head_loss_noalloc"]
+           "burst_lm_head_static_scratch_bytes", "burst_lm_head_tile_plan", "burst_lm_head_loss_noalloc",
+           "burst_attn_rope", "burst_attn_cache_append", "burst_attn_decode_workspace_bytes", "burst_attn_decode"]
 
 
 class BurstError(RuntimeError):
@@ -407,6 +432,129 @@ def burst_lm_head_tile_plan(shp):
     out = (C.c_int32 * 6)()
     _check(_lib.burst_lm_head_tile_plan(C.byref(shp), out))
     return [tuple(out[2 * i:2 * i + 2]) for i in range(3)]
+
+
+def _check_device(*tensors):
+    """Kernels run on the current device, on which the stream must be: tensors of another one are refused."""
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != current):
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{current}")
+
+
+def _int32(t, dims):
+    if t.dtype != torch.int32 or t.dim() != dims or (t.numel() > 0 and t.size(-1) > 1 and t.stride(-1) != 1):
+        raise ValueError(f"int32 tensor of {dims} dimensions with a contiguous last one expected")
+    return t.data_ptr()
+
+
+def rope(positions, inv_freq, rotary_dim=None, adjacent=False, axis_of_pair=None):
+    """A rotation: positions [axes, batch, rows] int32, inv_freq [rotary_dim / 2] fp32, the axis of each pair (default: the first).  A
+    plan that a program keeps: it holds the two tensors, whose contents are read when a call that uses it runs."""
+    _check_device(positions, inv_freq)
+    pairs = inv_freq.numel()
+    if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or (rotary_dim is not None and rotary_dim != 2 * pairs):
+        raise ValueError("inv_freq: rotary_dim / 2 contiguous fp32 numbers expected")
+    axes = [0] * pairs if axis_of_pair is None else [int(a) for a in axis_of_pair]
+    if len(axes) != pairs or not all(0 <= a < positions.size(0) for a in axes):
+        raise ValueError("axis_of_pair: an axis of positions for each pair expected")
+    if pairs > 64:
+        raise ValueError("at most 64 pairs")
+    r = burst_rope_t(positions.size(0), 2 * pairs, int(adjacent), 0, inv_freq.data_ptr(), _int32(positions, 3),
+                     positions.stride(0), positions.stride(1), (C.c_uint8 * 64)(*axes))
+    r._tensors = (positions, inv_freq)
+    return r
+
+
+def _check_positions(shp, r):
+    if r is not None and tuple(r._tensors[0].shape[1:]) != (shp.batch, shp.sq):
+        raise ValueError(f"positions of {shp.batch} sequences of {shp.sq} rows expected, not {tuple(r._tensors[0].shape[1:])}")
+
+
+def _check_sizes(t, *sizes):
+    if t is not None and tuple(t.shape) != sizes:
+        raise ValueError(f"tensor of {sizes} expected, not {tuple(t.shape)}")
+
+
+def burst_attn_rope(shp, rope, q, q_out, k=None, k_out=None, inverse=False, stream=None):
+    """q, q_out [batch, sq, q_heads, head_dim], k, k_out [batch, sq, kv_heads, head_dim], bf16 or fp32; q_out may be q (in place)."""
+    _check_device(q, q_out, k, k_out)
+    _check_positions(shp, rope)
+    for t, heads in ((q, shp.q_heads), (q_out, shp.q_heads), (k, shp.kv_heads), (k_out, shp.kv_heads)):
+        _check_sizes(t, shp.batch, shp.sq, heads, shp.head_dim)
+    _check(_lib.burst_attn_rope(C.byref(shp), C.byref(rope), _ref(tensor(q)), _ref(tensor(q_out)), _ref(tensor(k)),
+                                _ref(tensor(k_out)), int(inverse), _stream(stream)))
+
+
+def paged_cache(k, v, table, rows, k_scale=None, v_scale=None):
+    """A paged cache: k and v [pages, page_rows, kv_heads, head_dim] (bf16 or float8_e4m3fn, in any order of memory), table int32
+    [batch, pages of a sequence], rows int32 [batch], scales fp32 [kv_heads].  A handle that a program keeps; it holds the tensors."""
+    _check_device(k, v, table, rows, k_scale, v_scale)
+    if k.shape != v.shape or k.dim() != 4 or table.dim() != 2 or rows.dim() != 1 or table.size(0) != rows.size(0):
+        raise ValueError("k and v [pages, page_rows, kv_heads, head_dim], table [batch, pages], rows [batch] expected")
+    if rows.numel() > 1 and rows.stride(0) != 1:
+        raise ValueError("rows: contiguous numbers expected")
+    for s in (k_scale, v_scale):
+        if s is not None and (s.dtype != torch.float32 or not s.is_contiguous() or s.numel() != k.size(2)):
+            raise ValueError("scales: kv_heads contiguous fp32 numbers expected")
+    c = burst_cache_t(_cache_tensor(k), _cache_tensor(v), k.size(0), k.size(1), table.size(1), _int32(table, 2), table.stride(0),
+                      _int32(rows, 1), None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
+    c._tensors = (k, v, table, rows, k_scale, v_scale)
+    return c
+
+
+def _cache_tensor(t):
+    if t.stride(3) != 1:
+        raise ValueError("head_dim must be contiguous")
+    return burst_tensor_t(t.data_ptr(), {torch.bfloat16: BURST_BF16, torch.float8_e4m3fn: BURST_F8E4M3}[t.dtype], 0, t.stride(0),
+                          t.stride(1), t.stride(2))
+
+
+def _check_cache(shp, cache):
+    k, _, _, rows, _, _ = cache._tensors
+    if rows.size(0) != shp.batch or k.size(2) != shp.kv_heads or k.size(3) != shp.head_dim:
+        raise ValueError("the cache has another batch, kv_heads or head_dim than the shape")
+
+
+def _numbers(t, shp):
+    """The address of an int32 number for each sequence, or None."""
+    if t is None:
+        return None
+    _check_device(t)
+    _check_sizes(t, shp.batch)
+    return _int32(t, 1)
+
+
+def burst_attn_cache_append(shp, cache, k, v, new_rows=None, rope=None, q=None, q_out=None, stream=None):
+    """k, v [batch, sq, kv_heads, head_dim] bf16: sequence b's first new_rows[b] rows (all) become its rows rows[b] - new_rows[b] ..
+    rows[b] - 1.  With a rotation the keys are turned, and q [batch, sq, q_heads, head_dim] into q_out."""
+    _check_device(k, v, q, q_out)
+    _check_cache(shp, cache)
+    _check_positions(shp, rope)
+    for t, heads in ((k, shp.kv_heads), (v, shp.kv_heads), (q, shp.q_heads), (q_out, shp.q_heads)):
+        _check_sizes(t, shp.batch, shp.sq, heads, shp.head_dim)
+    _check(_lib.burst_attn_cache_append(C.byref(shp), C.byref(cache), _ref(tensor(k)), _ref(tensor(v)), _numbers(new_rows, shp),
+                                        _ref(rope), _ref(tensor(q)), _ref(tensor(q_out)), _stream(stream)))
+
+
+def burst_attn_decode_workspace_bytes(shp):
+    n = _lib.burst_attn_decode_workspace_bytes(C.byref(shp))
+    if n < 0:
+        raise BurstError(BURST_ERR_INVALID_ARG)
+    return n
+
+
+def burst_attn_decode(shp, cache, q, o, lse=None, workspace=None, first_row=None, stream=None):
+    """q [batch, 1, q_heads, head_dim] bf16 over the cache's rows from first_row[b] on: o (bf16 or fp32), lse [batch, q_heads, 1].
+    shp.sk bounds the rows of a sequence; workspace: a one-byte tensor of burst_attn_decode_workspace_bytes(shp) bytes."""
+    _check_device(q, o, lse, workspace)
+    _check_cache(shp, cache)
+    _check_sizes(q, shp.batch, 1, shp.q_heads, shp.head_dim)
+    _check_sizes(o, shp.batch, 1, shp.q_heads, shp.head_dim)
+    _check_sizes(lse, shp.batch, shp.q_heads, 1)
+    ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(_lib.burst_attn_decode(C.byref(shp), C.byref(cache), _ref(tensor(q)), _numbers(first_row, shp), _ref(tensor(o)),
+                                  _ref(rowvec(lse)), ws, n, _stream(stream)))
 
 
 def burst_attn_mfma_probe(random_operands, iterations, stream=None):

@@ -8,7 +8,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libburstattn.so")
-SOURCES = ["api.hip", "fwd.hip", "bwd.hip", "elementwise.hip", "lm_head.hip"]
+SOURCES = ["api.hip", "fwd.hip", "bwd.hip", "elementwise.hip", "lm_head.hip", "rotary.hip", "decode.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffast-math", "-fno-finite-math-only",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]

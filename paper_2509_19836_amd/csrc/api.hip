@@ -9,8 +9,10 @@
 #include <mutex>
 
 #include "../../include/burst_attn.h"
+#include "../../include/burst_attn_cache.h"
 #include "../../include/burst_attn_diag.h"
 #include "../../include/burst_lm_head.h"
+#include "cache.hpp"
 #include "kernels.hpp"
 #include "spans.hpp"
 
@@ -297,6 +299,85 @@ int check_bwd(const burst_shape_t* shape, const burst_tensor_t* q, const burst_t
   return BURST_OK;
 }
 
+constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 1;   // batch * rows of a rotation or an append: 32-bit token numbers
+
+// An array of 32-bit numbers in device memory.
+bool aligned4(const void* ptr) { return ptr && ((uintptr_t)ptr & 3) == 0; }
+
+int check_rope(const burst_rope_t* r, const burst_shape_t* shape, int32_t inverse, RopeDev* out) {
+  std::memset(out, 0, sizeof(*out));
+  if (!r || r->n_axes < 1 || r->n_axes > BURST_ROPE_MAX_AXES) return BURST_ERR_INVALID_ARG;
+  if (r->rotary_dim < 1 || r->rotary_dim > shape->head_dim || (r->rotary_dim & 1)) return BURST_ERR_INVALID_ARG;
+  if (r->rotary_dim % 16) return BURST_ERR_UNSUPPORTED;   // a thread turns 8 pairs
+  if (!aligned4(r->inv_freq) || !aligned4(r->positions) || r->stride_axis < 0 || r->stride_b < 0) return BURST_ERR_INVALID_ARG;
+  if (r->stride_axis > INT64_MAX / 8 || r->stride_b > (INT64_MAX / 4) / shape->batch) return BURST_ERR_INVALID_ARG;
+  for (int i = 0; i < r->rotary_dim / 2; ++i) {
+    if (r->axis_of_pair[i] >= r->n_axes) return BURST_ERR_INVALID_ARG;
+    out->axes[i / 8] |= (uint16_t)(r->axis_of_pair[i] << (2 * (i % 8)));
+  }
+  out->inv_freq = r->inv_freq;
+  out->positions = r->positions;
+  out->s_axis = r->stride_axis;
+  out->s_b = r->stride_b;
+  out->n_axes = r->n_axes;
+  out->rotary_dim = r->rotary_dim;
+  out->adjacent = r->adjacent != 0;
+  out->inverse = inverse != 0;
+  return BURST_OK;
+}
+
+// Input and output of a rotation: one memory, if at all, only as the same tensor.
+int check_turned(const burst_tensor_t* x, const burst_tensor_t* y, int types_in, int types_out, const burst_shape_t* s, int64_t heads,
+                 TensorDev* in, TensorDev* out) {
+  BURST_TRY(check_tensor(x, types_in, in));
+  BURST_TRY(check_tensor(y, types_out, out));
+  BURST_TRY(check_no_overlap(*out, s->batch, s->sq, heads, s->head_dim));
+  if (x->ptr == y->ptr && (x->dtype != y->dtype || x->stride_b != y->stride_b || x->stride_s != y->stride_s || x->stride_h != y->stride_h))
+    return BURST_ERR_INVALID_ARG;
+  return BURST_OK;
+}
+
+int check_cache(const burst_cache_t* c, const burst_shape_t* shape, CacheDev* out) {
+  std::memset(out, 0, sizeof(*out));
+  if (!c || !c->k.ptr || !c->v.ptr) return BURST_ERR_INVALID_ARG;
+  for (const burst_tensor_t* t : {&c->k, &c->v}) {
+    if (t->dtype != BURST_BF16 && t->dtype != BURST_F32 && t->dtype != BURST_F8E4M3) return BURST_ERR_INVALID_ARG;
+    if (t->dtype == BURST_F32) return BURST_ERR_UNSUPPORTED;
+    const int64_t unit = t->dtype == BURST_BF16 ? 8 : 16;
+    if (((uintptr_t)t->ptr) & 15) return BURST_ERR_INVALID_ARG;
+    if (t->stride_b < 0 || t->stride_s < 0 || t->stride_h < 0 || t->stride_b % unit || t->stride_s % unit || t->stride_h % unit)
+      return BURST_ERR_INVALID_ARG;
+    if (t->stride_s > kMaxRowStride) return BURST_ERR_UNSUPPORTED;   // 32-bit offsets inside a tile of rows
+  }
+  if (c->k.dtype != c->v.dtype || c->k.stride_b != c->v.stride_b || c->k.stride_s != c->v.stride_s || c->k.stride_h != c->v.stride_h)
+    return BURST_ERR_UNSUPPORTED;   // (one address for a row of both)
+  if (c->n_pages < 1 || c->page_rows < 1 || c->table_cols < 1) return BURST_ERR_INVALID_ARG;
+  if (c->n_pages > INT32_MAX || c->page_rows > (1 << 20) || (int64_t)c->table_cols * c->page_rows > kMaxRows) return BURST_ERR_UNSUPPORTED;
+  // offsets stay far inside 64 bits
+  if (c->k.stride_b > ((int64_t)1 << 60) / c->n_pages || c->k.stride_h > ((int64_t)1 << 60) / shape->kv_heads) return BURST_ERR_INVALID_ARG;
+  if (!aligned4(c->table) || !aligned4(c->rows)) return BURST_ERR_INVALID_ARG;
+  if (c->table_stride != 0 && (c->table_stride < c->table_cols || c->table_stride > ((int64_t)1 << 60) / shape->batch))
+    return BURST_ERR_INVALID_ARG;
+  for (const float* scale : {c->k_scale, c->v_scale})
+    if (scale && (c->k.dtype == BURST_BF16 || !aligned4(scale))) return BURST_ERR_INVALID_ARG;
+  out->k = c->k.ptr;
+  out->v = c->v.ptr;
+  out->s_page = c->k.stride_b;
+  out->s_row = c->k.stride_s;
+  out->s_head = c->k.stride_h;
+  out->is_f8 = c->k.dtype == BURST_F8E4M3;
+  out->n_pages = (int32_t)c->n_pages;
+  out->page_rows = c->page_rows;
+  out->table_cols = c->table_cols;
+  out->table = c->table;
+  out->table_stride = c->table_stride;
+  out->rows = c->rows;
+  out->k_scale = c->k_scale;
+  out->v_scale = c->v_scale;
+  out->by_page.init((uint32_t)c->page_rows);
+  return BURST_OK;
+}
+
 // Steps of one query chunk: those without keys (or queries) contribute nothing, the others run.
 hipError_t run_bwd(const BwdParams& p0, const BwdStep* steps, int n, hipStream_t stream) {
   BwdParams p = p0;
@@ -487,6 +568,97 @@ int burst_attn_steps_bwd(int32_t n_steps, const burst_shape_t* shapes, const bur
   }
   return BURST_OK;
 } BURST_NO_THROW
+
+int burst_attn_rope(const burst_shape_t* shape, const burst_rope_t* rope, const burst_tensor_t* q, const burst_tensor_t* q_out,
+                    const burst_tensor_t* k, const burst_tensor_t* k_out, int32_t inverse, void* hip_stream) {
+  BURST_TRY(check_shape(shape));
+  RopeParams p;
+  std::memset(&p, 0, sizeof(p));
+  BURST_TRY(check_rope(rope, shape, inverse, &p.rope));
+  BURST_TRY(check_turned(q, q_out, 3, 3, shape, shape->q_heads, &p.q, &p.q_out));
+  if ((k == nullptr) != (k_out == nullptr)) return BURST_ERR_INVALID_ARG;
+  if (k) BURST_TRY(check_turned(k, k_out, 3, 3, shape, shape->kv_heads, &p.k, &p.k_out));
+  if (k && k_out->ptr == q_out->ptr) return BURST_ERR_INVALID_ARG;
+  if (shape->sq > kMaxTokens / shape->batch) return BURST_ERR_UNSUPPORTED;
+  p.batch = shape->batch;
+  p.sq = (int32_t)shape->sq;
+  p.q_heads = shape->q_heads;
+  p.kv_heads = shape->kv_heads;
+  p.head_dim = shape->head_dim;
+  const hipError_t e = launch_rope(p, (hipStream_t)hip_stream);
+  return e == hipSuccess ? BURST_OK : hip_fail(e);
+}
+
+int burst_attn_cache_append(const burst_shape_t* shape, const burst_cache_t* cache, const burst_tensor_t* k, const burst_tensor_t* v,
+                            const int32_t* new_rows, const burst_rope_t* rope, const burst_tensor_t* q, const burst_tensor_t* q_out,
+                            void* hip_stream) {
+  BURST_TRY(check_shape(shape));
+  AppendParams p;
+  std::memset(&p, 0, sizeof(p));
+  BURST_TRY(check_cache(cache, shape, &p.cache));
+  // what is written must not be written twice: nor k's rows as v's
+  const TensorDev pages{p.cache.k, p.cache.s_page, p.cache.s_row, p.cache.s_head, 0};
+  BURST_TRY(check_no_overlap(pages, p.cache.n_pages, p.cache.page_rows, shape->kv_heads, shape->head_dim));
+  if (p.cache.k == p.cache.v) return BURST_ERR_INVALID_ARG;
+  BURST_TRY(check_tensor(k, 1, &p.k));
+  BURST_TRY(check_tensor(v, 1, &p.v));
+  if (new_rows && !aligned4(new_rows)) return BURST_ERR_INVALID_ARG;
+  if (rope) BURST_TRY(check_rope(rope, shape, 0, &p.rope));
+  if ((q == nullptr) != (q_out == nullptr)) return BURST_ERR_INVALID_ARG;
+  if (q && !rope) return BURST_ERR_INVALID_ARG;   // nothing to be done to it
+  if (q) BURST_TRY(check_turned(q, q_out, 1, 1, shape, shape->q_heads, &p.q, &p.q_out));
+  if (shape->sq > kMaxTokens / shape->batch) return BURST_ERR_UNSUPPORTED;
+  p.new_rows = new_rows;
+  p.batch = shape->batch;
+  p.sq = (int32_t)shape->sq;
+  p.q_heads = shape->q_heads;
+  p.kv_heads = shape->kv_heads;
+  p.head_dim = shape->head_dim;
+  const hipError_t e = launch_cache_append(p, (hipStream_t)hip_stream);
+  return e == hipSuccess ? BURST_OK : hip_fail(e);
+}
+
+static int check_decode_shape(const burst_shape_t* shape) {
+  BURST_TRY(check_shape(shape));
+  if (shape->sq != 1) return BURST_ERR_INVALID_ARG;
+  // 32-bit numbers of (sequence, head) pairs and of units of work
+  if ((int64_t)shape->batch * shape->q_heads > (1 << 24)) return BURST_ERR_UNSUPPORTED;
+  return BURST_OK;
+}
+
+int64_t burst_attn_decode_workspace_bytes(const burst_shape_t* shape) {
+  if (check_decode_shape(shape) != BURST_OK) return -1;
+  return decode_workspace_bytes(shape->batch, shape->q_heads, shape->kv_heads, shape->head_dim, shape->sk);
+}
+
+int burst_attn_decode(const burst_shape_t* shape, const burst_cache_t* cache, const burst_tensor_t* q, const int32_t* first_row,
+                      const burst_tensor_t* o, const burst_rowvec_t* lse, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  BURST_TRY(check_decode_shape(shape));
+  DecodeParams p;
+  std::memset(&p, 0, sizeof(p));
+  BURST_TRY(check_cache(cache, shape, &p.cache));
+  if (shape->sk > (int64_t)p.cache.table_cols * p.cache.page_rows) return BURST_ERR_INVALID_ARG;
+  BURST_TRY(check_tensor(q, 1, &p.q));
+  BURST_TRY(check_tensor(o, 3, &p.o));
+  BURST_TRY(check_no_overlap(p.o, shape->batch, 1, shape->q_heads, shape->head_dim));
+  if (lse) {
+    BURST_TRY(check_rowvec(lse, &p.lse));
+    BURST_TRY(check_rowvec_no_overlap(p.lse, shape->batch, shape->q_heads, 1));
+  }
+  if (first_row && !aligned4(first_row)) return BURST_ERR_INVALID_ARG;
+  const int64_t need = decode_workspace_bytes(shape->batch, shape->q_heads, shape->kv_heads, shape->head_dim, shape->sk);
+  if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return BURST_ERR_INVALID_ARG;
+  p.first_row = first_row;
+  p.batch = shape->batch;
+  p.q_heads = shape->q_heads;
+  p.kv_heads = shape->kv_heads;
+  p.head_dim = shape->head_dim;
+  p.max_rows = (int32_t)shape->sk;
+  p.scale = shape->scale;
+  p.workspace = workspace;
+  const hipError_t e = launch_decode(p, (hipStream_t)hip_stream);
+  return e == hipSuccess ? BURST_OK : hip_fail(e);
+}
 
 static int fill_common(int32_t dev_i, int32_t shard_j, int32_t G, int64_t N, burst_mask_t* out) {
   if (!out || G < 1 || dev_i < 0 || dev_i >= G || shard_j < 0 || shard_j >= G || N < 0) return BURST_ERR_INVALID_ARG;

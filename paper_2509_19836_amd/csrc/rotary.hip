@@ -1,0 +1,254 @@
+// The rotation by positions, on its own (queries and keys, or their gradients) and on the way into a paged cache.
+//
+// A head is cut into slots of 16 elements, one for a thread: 8 pairs of it (two runs of 8 elements that lie rotary_dim / 2 apart, or 16 in
+// a row where pairs are neighbours), or 16 elements behind the rotated ones, which are copied.  Angle, sine and cosine of a pair
+// depend on the token alone: a thread forms them once and takes them through its share of the token's heads, so the kernels stay bound by the
+// bytes they move.
+#include "cache.hpp"
+#include "kernels.hpp"
+
+namespace burst {
+
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4u;   // 4-byte aligned in memory
+
+struct Turn {
+  float c[8], s[8];
+};
+
+// Sine and cosine of the 8 pairs of a slot at one token.  The angle in whole turns, position * inv_freq / 2 pi, is formed in 64 bits:
+// 2^31 positions leave 1e-7 of a turn, where 32 bits would lose the place on the circle from about 10^5 on.  What is left of
+// it after the whole turns, and then after the quarter turns, is within +-pi / 4, where the Taylor series of sine to x^9 and
+// cosine to x^10 are off by less than 2e-9 and 3e-10.
+__device__ __forceinline__ void turn_of(const RopeDev& r, int slot, int32_t b, int32_t row, Turn& t) {
+  int32_t pos[3];
+#pragma unroll
+  for (int a = 0; a < 3; ++a) pos[a] = a < r.n_axes ? r.positions[a * r.s_axis + b * r.s_b + row] : 0;
+  const f32x4u f0 = *reinterpret_cast<const f32x4u*>(r.inv_freq + 8 * slot);
+  const f32x4u f1 = *reinterpret_cast<const f32x4u*>(r.inv_freq + 8 * slot + 4);
+  const uint32_t axes = r.axes[slot];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t a = (axes >> (2 * j)) & 3u;
+    const int32_t p = a == 0 ? pos[0] : a == 1 ? pos[1] : pos[2];
+    double turns = (double)p * (double)(j < 4 ? f0[j & 3] : f1[j & 3]) * 0.15915494309189533577;   // 1 / 2 pi
+    turns -= rint(turns);
+    const float x = (float)turns, quarter = rintf(4.f * x);
+    const float y = fmaf(-0.25f, quarter, x) * 6.28318530717958648f, z = y * y;
+    const float sy = fmaf(y * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), y);
+    const float cy = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+    const int n = (int)quarter;
+    const float s = n & 1 ? cy : sy, c = n & 1 ? sy : cy;
+    t.s[j] = ((n & 2) != 0) != (r.inverse != 0) ? -s : s;
+    t.c[j] = (n + 1) & 2 ? -c : c;
+  }
+}
+
+// The two runs of 8 elements of a thread's slot, from the head's first element.
+struct SlotPlace {
+  int lo, hi;
+  bool turned;
+  __device__ __forceinline__ void init(const RopeDev& r, int slot) {
+    turned = 16 * slot < r.rotary_dim;
+    const bool halves = turned && !r.adjacent;
+    lo = halves ? 8 * slot : 16 * slot;
+    hi = halves ? 8 * slot + r.rotary_dim / 2 : 16 * slot + 8;
+  }
+};
+
+// 16 elements as they lie in memory.
+template <bool F32>
+struct Raw {
+  u32x4 w[F32 ? 4 : 2];
+  __device__ __forceinline__ void load(const void* ptr, int64_t off, const SlotPlace& at) {
+    if constexpr (F32) {
+      const float* x = (const float*)ptr + off;
+      w[0] = *reinterpret_cast<const u32x4*>(x + at.lo);
+      w[1] = *reinterpret_cast<const u32x4*>(x + at.lo + 4);
+      w[2] = *reinterpret_cast<const u32x4*>(x + at.hi);
+      w[3] = *reinterpret_cast<const u32x4*>(x + at.hi + 4);
+    } else {
+      const __bf16* x = (const __bf16*)ptr + off;
+      w[0] = *reinterpret_cast<const u32x4*>(x + at.lo);
+      w[1] = *reinterpret_cast<const u32x4*>(x + at.hi);
+    }
+  }
+  __device__ __forceinline__ float value(int i) const {   // (i is known when compiled)
+    const uint32_t word = F32 ? w[i / 4][i % 4] : w[i / 8][i % 8 / 2];   // (a bit cast of w[..][..] itself would take the vector's first word)
+    return __builtin_bit_cast(float, F32 ? word : i & 1 ? word & 0xffff0000u : word << 16);
+  }
+};
+
+// Where 16 results go: fp32, bf16, or e4m3 over a scale.
+enum class To { kF32, kBf16, kF8 };
+template <To TO>
+__device__ __forceinline__ void store16(void* ptr, int64_t off, const SlotPlace& at, const float (&y)[16], float over_scale) {
+  if constexpr (TO == To::kF32) {
+    float* x = (float*)ptr + off;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(x + (i < 2 ? at.lo : at.hi) + 4 * (i & 1)) = f32x4{y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]};
+  } else if constexpr (TO == To::kBf16) {
+    __bf16* x = (__bf16*)ptr + off;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 z;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = (__bf16)y[8 * h + e];
+      *reinterpret_cast<bf16x8*>(x + (h ? at.hi : at.lo)) = z;
+    }
+  } else {
+    uint8_t* x = (uint8_t*)ptr + off;
+    float z[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float s = y[i] * over_scale;
+      z[i] = s != s ? s : fminf(fmaxf(s, -448.f), 448.f);   // (the conversion itself makes NaN of what is too large)
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x2 out;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        int two = __builtin_amdgcn_cvt_pk_fp8_f32(z[8 * h + 4 * w], z[8 * h + 4 * w + 1], 0, false);
+        out[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[8 * h + 4 * w + 2], z[8 * h + 4 * w + 3], two, true);
+      }
+      *reinterpret_cast<u32x2*>(x + (h ? at.hi : at.lo)) = out;
+    }
+  }
+}
+
+// (what is not turned keeps its bits: no multiplication by 1 and 0, which a neighbour's infinity would make a NaN of)
+template <bool F32>
+__device__ __forceinline__ void turned(const Raw<F32>& raw, const Turn& t, bool adjacent, bool turn, float (&y)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = raw.value(i);
+  if (!turn) return;
+  if (adjacent) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float a = y[2 * j], b = y[2 * j + 1];
+      y[2 * j] = a * t.c[j] - b * t.s[j];
+      y[2 * j + 1] = b * t.c[j] + a * t.s[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float a = y[j], b = y[8 + j];
+      y[j] = a * t.c[j] - b * t.s[j];
+      y[8 + j] = b * t.c[j] + a * t.s[j];
+    }
+  }
+}
+
+// How a work-group of 256 threads is shared: 2^slots_log2 slots of a head, 2^heads_log2 heads side by side, the rest tokens.
+struct TokenShare {
+  int slots_log2, heads_log2;
+  __host__ __device__ __forceinline__ int tokens() const { return 256 >> (slots_log2 + heads_log2); }
+};
+
+// A thread's share of a token's heads.
+template <bool F32, To TO>
+__device__ __forceinline__ void turn_heads(const RopeDev& r, const Turn& t, const SlotPlace& at, const void* from, int64_t from_off,
+                                           int64_t from_sh, void* to, int64_t to_off, int64_t to_sh, int first, int step, int heads,
+                                           const float* scale) {
+  constexpr int U = F32 ? 2 : 4;   // heads whose loads are under way together
+  for (int h0 = first; h0 < heads; h0 += U * step) {
+    Raw<F32> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h0 + u * step < heads) raw[u].load(from, from_off + (h0 + u * step) * from_sh, at);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * step;
+      if (h < heads) {
+        float y[16];
+        turned(raw[u], t, r.adjacent != 0, at.turned, y);
+        store16<TO>(to, to_off + h * to_sh, at, y, TO == To::kF8 && scale ? 1.f / scale[h] : 1.f);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void turn_tensor(const RopeDev& r, const Turn& t, const SlotPlace& at, const TensorDev& x, const TensorDev& y,
+                                            int32_t b, int32_t row, int first, int step, int heads) {
+  const int64_t from = b * x.sb + row * x.ss, to = b * y.sb + row * y.ss;
+  if (x.is_f32) {
+    if (y.is_f32) turn_heads<true, To::kF32>(r, t, at, x.ptr, from, x.sh, y.ptr, to, y.sh, first, step, heads, nullptr);
+    else turn_heads<true, To::kBf16>(r, t, at, x.ptr, from, x.sh, y.ptr, to, y.sh, first, step, heads, nullptr);
+  } else {
+    if (y.is_f32) turn_heads<false, To::kF32>(r, t, at, x.ptr, from, x.sh, y.ptr, to, y.sh, first, step, heads, nullptr);
+    else turn_heads<false, To::kBf16>(r, t, at, x.ptr, from, x.sh, y.ptr, to, y.sh, first, step, heads, nullptr);
+  }
+}
+
+__global__ __launch_bounds__(256) void rope_kernel(RopeParams p, TokenShare share) {
+  const int slot = threadIdx.x & ((1 << share.slots_log2) - 1), step = 1 << share.heads_log2;
+  const int head = (threadIdx.x >> share.slots_log2) & (step - 1);
+  const int64_t token = (int64_t)blockIdx.x * share.tokens() + (threadIdx.x >> (share.slots_log2 + share.heads_log2));
+  if (token >= (int64_t)p.batch * p.sq) return;
+  const int32_t b = (int32_t)token / p.sq, row = (int32_t)token - b * p.sq;   // (batch * sq < 2^31, checked on the host)
+  SlotPlace at;
+  at.init(p.rope, slot);
+  Turn t;
+  if (at.turned) turn_of(p.rope, slot, b, row, t);
+  turn_tensor(p.rope, t, at, p.q, p.q_out, b, row, head, step, p.q_heads);
+  if (p.k.ptr) turn_tensor(p.rope, t, at, p.k, p.k_out, b, row, head, step, p.kv_heads);
+}
+
+static TokenShare token_share(int32_t head_dim, int32_t heads) {
+  TokenShare s{head_dim == 128 ? 3 : 2, 0};
+  while (s.slots_log2 + s.heads_log2 < 8 && (4 << s.heads_log2) < heads) ++s.heads_log2;
+  return s;
+}
+
+hipError_t launch_rope(const RopeParams& p, hipStream_t stream) {
+  const int64_t total = (int64_t)p.batch * p.sq;
+  if (total == 0) return hipSuccess;
+  const TokenShare share = token_share(p.head_dim, p.q_heads);
+  const int64_t grid = (total + share.tokens() - 1) / share.tokens();
+  hipLaunchKernelGGL(rope_kernel, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
+  return hipGetLastError();
+}
+
+// A token's keys (turned) and values into its row of the cache, and its queries (turned) to q_out.
+__global__ __launch_bounds__(256) void cache_append_kernel(AppendParams p, TokenShare share) {
+  const int slot = threadIdx.x & ((1 << share.slots_log2) - 1), step = 1 << share.heads_log2;
+  const int head = (threadIdx.x >> share.slots_log2) & (step - 1);
+  const int64_t token = (int64_t)blockIdx.x * share.tokens() + (threadIdx.x >> (share.slots_log2 + share.heads_log2));
+  if (token >= (int64_t)p.batch * p.sq) return;
+  const int32_t b = (int32_t)token / p.sq, i = (int32_t)token - b * p.sq;
+  int32_t fresh = p.new_rows ? p.new_rows[b] : p.sq;
+  fresh = fresh < 0 ? 0 : fresh > p.sq ? p.sq : fresh;
+  if (i >= fresh) return;
+  SlotPlace at, as_is;
+  at.init(p.rope, slot);
+  as_is = SlotPlace{16 * slot, 16 * slot + 8, false};
+  Turn t;
+  if (at.turned) turn_of(p.rope, slot, b, i, t);
+  if (p.q.ptr)
+    turn_heads<false, To::kBf16>(p.rope, t, at, p.q.ptr, b * p.q.sb + i * p.q.ss, p.q.sh, p.q_out.ptr, b * p.q_out.sb + i * p.q_out.ss,
+                                 p.q_out.sh, head, step, p.q_heads, nullptr);
+  const int32_t row = p.cache.rows_of(b) - fresh + i;
+  const int64_t to = row < 0 ? -1 : p.cache.row_offset(b, row);
+  if (to < 0) return;
+  const int64_t k = b * p.k.sb + i * p.k.ss, v = b * p.v.sb + i * p.v.ss;
+  if (p.cache.is_f8) {
+    turn_heads<false, To::kF8>(p.rope, t, at, p.k.ptr, k, p.k.sh, p.cache.k, to, p.cache.s_head, head, step, p.kv_heads, p.cache.k_scale);
+    turn_heads<false, To::kF8>(p.rope, t, as_is, p.v.ptr, v, p.v.sh, p.cache.v, to, p.cache.s_head, head, step, p.kv_heads, p.cache.v_scale);
+  } else {
+    turn_heads<false, To::kBf16>(p.rope, t, at, p.k.ptr, k, p.k.sh, p.cache.k, to, p.cache.s_head, head, step, p.kv_heads, nullptr);
+    turn_heads<false, To::kBf16>(p.rope, t, as_is, p.v.ptr, v, p.v.sh, p.cache.v, to, p.cache.s_head, head, step, p.kv_heads, nullptr);
+  }
+}
+
+hipError_t launch_cache_append(const AppendParams& p, hipStream_t stream) {
+  const int64_t total = (int64_t)p.batch * p.sq;
+  if (total == 0) return hipSuccess;
+  const TokenShare share = token_share(p.head_dim, p.q.ptr ? p.q_heads : p.kv_heads);
+  const int64_t grid = (total + share.tokens() - 1) / share.tokens();
+  hipLaunchKernelGGL(cache_append_kernel, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
+  return hipGetLastError();
+}
+
+}  // namespace burst
