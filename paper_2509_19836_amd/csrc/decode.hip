@@ -9,7 +9,8 @@
 //   D / 16 elements of V, and one v_perm for every two of them makes them the A operand whose k index is the key: the keys that S^T leaves
 //   in this lane's accumulators (16 (e / 4) + 4g + e % 4), so P needs no exchange between lanes either.
 //   The running maximum of a column is a whole number (base 2), so that a rescale by 2^n changes no bit of P and O, and which
-//   rows another wave or work-group took has no influence but the order of fp32 sums.  P goes in as two bf16 numbers, truncated and rest.
+//   rows another wave or work-group took has no influence but the order of fp32 sums.  P goes in whole, as the three bf16 numbers that its
+//   24 bits are; the matrix pipe has the time for it.
 //
 //   Work is cut into units of 128 rows (a tile for each wave), numbered over (sequence, key head, rows), and dealt evenly to as many
 //   work-groups as the chip holds at once, whatever the sequences' lengths are: each finds its first unit by a scan over
@@ -335,7 +336,7 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
       }
       // this lane's keys: bit 16 (e / 4) + 4g + e % 4
       const uint32_t bits = ((seen >> (4 * g)) & 15u) | ((seen >> (4 * g + 12)) & 0xf0u);
-      bf16x8 p_hi[NC], p_lo[NC];
+      bf16x8 p_part[NC][3];
 #pragma unroll
       for (int nc = 0; nc < NC; ++nc) {
         float x[8], top = -INFINITY;
@@ -357,19 +358,21 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
           for (int j = 0; j < DT; ++j) acc[nc][j] *= f;
         }
         const float base = m[nc] == -INFINITY ? 0.f : m[nc];
-        uint32_t hi[4];
-        float lo[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           x[e] = __builtin_amdgcn_exp2f(x[e] - base);
           l[nc] += x[e];
-          lo[e] = x[e] - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[e]) & 0xffff0000u);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          hi[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x[2 * i + 1]), __builtin_bit_cast(uint32_t, x[2 * i]), 0x07060302u);
-        p_hi[nc] = __builtin_bit_cast(bf16x8, u32x4{hi[0], hi[1], hi[2], hi[3]});
-        p_lo[nc] = bf16x8{(__bf16)lo[0], (__bf16)lo[1], (__bf16)lo[2], (__bf16)lo[3], (__bf16)lo[4], (__bf16)lo[5], (__bf16)lo[6], (__bf16)lo[7]};
+        for (int part = 0; part < 3; ++part) {
+          u32x4 words;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            words[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x[2 * i + 1]), __builtin_bit_cast(uint32_t, x[2 * i]), 0x07060302u);
+          p_part[nc][part] = __builtin_bit_cast(bf16x8, words);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[e]) & 0xffff0000u);   // (exact)
+        }
       }
       // rows that are not seen may hold NaN, which a P of 0 would not silence
       if (seen != ~0u) {
@@ -400,8 +403,8 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
         const bf16x8 av = __builtin_bit_cast(bf16x8, a);
 #pragma unroll
         for (int nc = 0; nc < NC; ++nc) {
-          acc[nc][j] = mfma16(av, p_hi[nc], acc[nc][j]);
-          acc[nc][j] = mfma16(av, p_lo[nc], acc[nc][j]);
+#pragma unroll
+          for (int part = 0; part < 3; ++part) acc[nc][j] = mfma16(av, p_part[nc][part], acc[nc][j]);
         }
       }
       if (more) load_v(now);

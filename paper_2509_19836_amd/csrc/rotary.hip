@@ -16,10 +16,10 @@ struct Turn {
   float c[8], s[8];
 };
 
-// Sine and cosine of the 8 pairs of a slot at one token.  The angle in whole turns, position * inv_freq / 2 pi, is formed in 64 bits:
-// 2^31 positions leave 1e-7 of a turn, where 32 bits would lose the place on the circle from about 10^5 on.  What is left of
-// it after the whole turns, and then after the quarter turns, is within +-pi / 4, where the Taylor series of sine to x^9 and
-// cosine to x^10 are off by less than 2e-9 and 3e-10.
+// Sine and cosine of the 8 pairs of a slot at one token, rounded to fp32 once.  The angle in whole turns, position * inv_freq / 2 pi, is
+// formed in 64 bits: 2^31 positions leave 1e-7 of a turn, where 32 bits would lose the place on the circle from about 10^5 on.
+// What is left of it after the whole turns, and then after the quarter turns, is within +-pi / 4, where the Taylor series of sine to
+// x^11 and cosine to x^10 are off by less than 1e-11 and 2e-10.
 __device__ __forceinline__ void turn_of(const RopeDev& r, int slot, int32_t b, int32_t row, Turn& t) {
   int32_t pos[3];
 #pragma unroll
@@ -33,10 +33,9 @@ __device__ __forceinline__ void turn_of(const RopeDev& r, int slot, int32_t b, i
     const int32_t p = a == 0 ? pos[0] : a == 1 ? pos[1] : pos[2];
     double turns = (double)p * (double)(j < 4 ? f0[j & 3] : f1[j & 3]) * 0.15915494309189533577;   // 1 / 2 pi
     turns -= rint(turns);
-    const float x = (float)turns, quarter = rintf(4.f * x);
-    const float y = fmaf(-0.25f, quarter, x) * 6.28318530717958648f, z = y * y;
-    const float sy = fmaf(y * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), y);
-    const float cy = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+    const double quarter = rint(4. * turns), y = fma(-0.25, quarter, turns) * 6.28318530717958647693, z = y * y;
+    const float sy = (float)fma(y * z, fma(z, fma(z, fma(z, fma(z, -1. / 39916800., 1. / 362880.), -1. / 5040.), 1. / 120.), -1. / 6.), y);
+    const float cy = (float)fma(z, fma(z, fma(z, fma(z, fma(z, -1. / 3628800., 1. / 40320.), -1. / 720.), 1. / 24.), -0.5), 1.);
     const int n = (int)quarter;
     const float s = n & 1 ? cy : sy, c = n & 1 ? sy : cy;
     t.s[j] = ((n & 2) != 0) != (r.inverse != 0) ? -s : s;
@@ -82,7 +81,7 @@ struct Raw {
 // Where 16 results go: fp32, bf16, or e4m3 over a scale.
 enum class To { kF32, kBf16, kF8 };
 template <To TO>
-__device__ __forceinline__ void store16(void* ptr, int64_t off, const SlotPlace& at, const float (&y)[16], float over_scale) {
+__device__ __forceinline__ void store16(void* ptr, int64_t off, const SlotPlace& at, const float (&y)[16], float scale) {
   if constexpr (TO == To::kF32) {
     float* x = (float*)ptr + off;
 #pragma unroll
@@ -100,9 +99,11 @@ __device__ __forceinline__ void store16(void* ptr, int64_t off, const SlotPlace&
   } else {
     uint8_t* x = (uint8_t*)ptr + off;
     float z[16];
+    const float over = 1.f / scale;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float s = y[i] * over_scale;
+      // y / scale: the product with the reciprocal and what is left of y, as long as that is finite
+      const float near = y[i] * over, s = fabsf(near) < 1e4f ? fmaf(fmaf(-near, scale, y[i]), over, near) : near;
       z[i] = s != s ? s : fminf(fmaxf(s, -448.f), 448.f);   // (the conversion itself makes NaN of what is too large)
     }
 #pragma unroll
@@ -118,9 +119,12 @@ __device__ __forceinline__ void store16(void* ptr, int64_t off, const SlotPlace&
   }
 }
 
-// (what is not turned keeps its bits: no multiplication by 1 and 0, which a neighbour's infinity would make a NaN of)
+// Each product is rounded by itself, not one of the two fused into the difference: turning by a and by -a are then the same sums of the
+// same numbers, and elementary operations in 32 bits give the same result.
+// (What is not turned keeps its bits: no multiplication by 1 and 0, which a neighbour's infinity would make a NaN of.)
 template <bool F32>
 __device__ __forceinline__ void turned(const Raw<F32>& raw, const Turn& t, bool adjacent, bool turn, float (&y)[16]) {
+#pragma clang fp contract(off)
 #pragma unroll
   for (int i = 0; i < 16; ++i) y[i] = raw.value(i);
   if (!turn) return;
@@ -164,7 +168,7 @@ __device__ __forceinline__ void turn_heads(const RopeDev& r, const Turn& t, cons
       if (h < heads) {
         float y[16];
         turned(raw[u], t, r.adjacent != 0, at.turned, y);
-        store16<TO>(to, to_off + h * to_sh, at, y, TO == To::kF8 && scale ? 1.f / scale[h] : 1.f);
+        store16<TO>(to, to_off + h * to_sh, at, y, TO == To::kF8 && scale ? scale[h] : 1.f);
       }
     }
   }
