@@ -131,15 +131,16 @@ class burst_cache_t(C.Structure):
 
 
 _lib.burst_attn_rope.restype = C.c_int
-_lib.burst_attn_rope.argtypes = [_P(burst_shape_t), _P(burst_rope_t)] + [_P(burst_tensor_t)] * 4 + [C.c_int32, C.c_void_p]
+# (tensors of these calls go in as the bytes of their description)
+_lib.burst_attn_rope.argtypes = [_P(burst_shape_t), _P(burst_rope_t)] + [C.c_char_p] * 4 + [C.c_int32, C.c_void_p]
 _lib.burst_attn_cache_append.restype = C.c_int
-_lib.burst_attn_cache_append.argtypes = [_P(burst_shape_t), _P(burst_cache_t), _P(burst_tensor_t), _P(burst_tensor_t), C.c_void_p,
-                                         _P(burst_rope_t), _P(burst_tensor_t), _P(burst_tensor_t), C.c_void_p]
+_lib.burst_attn_cache_append.argtypes = [_P(burst_shape_t), _P(burst_cache_t), C.c_char_p, C.c_char_p, C.c_void_p,
+                                         _P(burst_rope_t), C.c_char_p, C.c_char_p, C.c_void_p]
 _lib.burst_attn_decode_workspace_bytes.restype = C.c_int64
 _lib.burst_attn_decode_workspace_bytes.argtypes = [_P(burst_shape_t)]
 _lib.burst_attn_decode.restype = C.c_int
-_lib.burst_attn_decode.argtypes = [_P(burst_shape_t), _P(burst_cache_t), _P(burst_tensor_t), C.c_void_p, _P(burst_tensor_t),
-                                   _P(burst_rowvec_t), C.c_void_p, C.c_int64, C.c_void_p]
+_lib.burst_attn_decode.argtypes = [_P(burst_shape_t), _P(burst_cache_t), C.c_char_p, C.c_void_p, C.c_char_p,
+                                   C.c_char_p, C.c_void_p, C.c_int64, C.c_void_p]
 _lib.burst_attn_status_string.restype = C.c_char_p
 _lib.burst_attn_status_string.argtypes = [C.c_int]
 _lib.burst_attn_last_hip_error.restype = C.c_int
@@ -434,12 +435,33 @@ def burst_lm_head_tile_plan(shp):
     return [tuple(out[2 * i:2 * i + 2]) for i in range(3)]
 
 
-def _check_device(*tensors):
-    """Kernels run on the current device, on which the stream must be: tensors of another one are refused."""
-    current = torch.cuda.current_device()
+def _current(stream):
+    """The stream to use (the current one, or a given one of the current device) and the number of its device."""
+    if stream is None:
+        s = torch.cuda.current_stream()
+        return s.cuda_stream, s.device_index
+    return stream, torch.cuda.current_device()
+
+
+def _check_device(device, *tensors):
+    """Kernels run on the current device: tensors that are elsewhere are refused."""
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != current):
-            raise ValueError(f"tensor on {t.device}, the current device is cuda:{current}")
+        if t is not None and t.get_device() != device:      # (-1: not on a GPU)
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
+
+
+_pack_tensor, _pack_rowvec = struct.Struct("=Qiiqqq").pack, struct.Struct("=Qqq").pack
+
+
+def _packed(t, device, *sizes):
+    """The bytes of the burst_tensor_t of a tensor of these sizes on this device, or None."""
+    if t is None:
+        return None
+    _check_device(device, t)
+    stride = t.stride()
+    if t.shape != sizes or stride[3] != 1:
+        raise ValueError(f"tensor of {sizes} with a contiguous last dimension expected, not {tuple(t.shape)}, strides {stride}")
+    return _pack_tensor(t.data_ptr(), _DTYPES[t.dtype], 0, stride[0], stride[1], stride[2])
 
 
 def _int32(t, dims):
@@ -451,7 +473,7 @@ def _int32(t, dims):
 def rope(positions, inv_freq, rotary_dim=None, adjacent=False, axis_of_pair=None):
     """A rotation: positions [axes, batch, rows] int32, inv_freq [rotary_dim / 2] fp32, the axis of each pair (default: the first).  A
     plan that a program keeps: it holds the two tensors, whose contents are read when a call that uses it runs."""
-    _check_device(positions, inv_freq)
+    _check_device(torch.cuda.current_device(), positions, inv_freq)
     pairs = inv_freq.numel()
     if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or (rotary_dim is not None and rotary_dim != 2 * pairs):
         raise ValueError("inv_freq: rotary_dim / 2 contiguous fp32 numbers expected")
@@ -466,30 +488,25 @@ def rope(positions, inv_freq, rotary_dim=None, adjacent=False, axis_of_pair=None
     return r
 
 
-def _check_positions(shp, r):
-    if r is not None and tuple(r._tensors[0].shape[1:]) != (shp.batch, shp.sq):
-        raise ValueError(f"positions of {shp.batch} sequences of {shp.sq} rows expected, not {tuple(r._tensors[0].shape[1:])}")
-
-
-def _check_sizes(t, *sizes):
-    if t is not None and tuple(t.shape) != sizes:
-        raise ValueError(f"tensor of {sizes} expected, not {tuple(t.shape)}")
+def _check_positions(r, batch, sq):
+    if r is not None and r._tensors[0].shape[1:] != (batch, sq):
+        raise ValueError(f"positions of {batch} sequences of {sq} rows expected, not {tuple(r._tensors[0].shape[1:])}")
 
 
 def burst_attn_rope(shp, rope, q, q_out, k=None, k_out=None, inverse=False, stream=None):
     """q, q_out [batch, sq, q_heads, head_dim], k, k_out [batch, sq, kv_heads, head_dim], bf16 or fp32; q_out may be q (in place)."""
-    _check_device(q, q_out, k, k_out)
-    _check_positions(shp, rope)
-    for t, heads in ((q, shp.q_heads), (q_out, shp.q_heads), (k, shp.kv_heads), (k_out, shp.kv_heads)):
-        _check_sizes(t, shp.batch, shp.sq, heads, shp.head_dim)
-    _check(_lib.burst_attn_rope(C.byref(shp), C.byref(rope), _ref(tensor(q)), _ref(tensor(q_out)), _ref(tensor(k)),
-                                _ref(tensor(k_out)), int(inverse), _stream(stream)))
+    stream, device = _current(stream)
+    batch, sq, q_heads, kv_heads, d = shp.batch, shp.sq, shp.q_heads, shp.kv_heads, shp.head_dim
+    _check_positions(rope, batch, sq)
+    _check(_lib.burst_attn_rope(shp, rope, _packed(q, device, batch, sq, q_heads, d), _packed(q_out, device, batch, sq, q_heads, d),
+                                _packed(k, device, batch, sq, kv_heads, d), _packed(k_out, device, batch, sq, kv_heads, d),
+                                int(inverse), stream))
 
 
 def paged_cache(k, v, table, rows, k_scale=None, v_scale=None):
     """A paged cache: k and v [pages, page_rows, kv_heads, head_dim] (bf16 or float8_e4m3fn, in any order of memory), table int32
     [batch, pages of a sequence], rows int32 [batch], scales fp32 [kv_heads].  A handle that a program keeps; it holds the tensors."""
-    _check_device(k, v, table, rows, k_scale, v_scale)
+    _check_device(torch.cuda.current_device(), k, v, table, rows, k_scale, v_scale)
     if k.shape != v.shape or k.dim() != 4 or table.dim() != 2 or rows.dim() != 1 or table.size(0) != rows.size(0):
         raise ValueError("k and v [pages, page_rows, kv_heads, head_dim], table [batch, pages], rows [batch] expected")
     if rows.numel() > 1 and rows.stride(0) != 1:
@@ -510,31 +527,32 @@ def _cache_tensor(t):
                           t.stride(1), t.stride(2))
 
 
-def _check_cache(shp, cache):
+def _check_cache(cache, batch, kv_heads, d):
     k, _, _, rows, _, _ = cache._tensors
-    if rows.size(0) != shp.batch or k.size(2) != shp.kv_heads or k.size(3) != shp.head_dim:
+    if rows.shape[0] != batch or k.shape[2:] != (kv_heads, d):
         raise ValueError("the cache has another batch, kv_heads or head_dim than the shape")
 
 
-def _numbers(t, shp):
+def _numbers(t, device, batch):
     """The address of an int32 number for each sequence, or None."""
     if t is None:
         return None
-    _check_device(t)
-    _check_sizes(t, shp.batch)
+    _check_device(device, t)
+    if t.shape != (batch,):
+        raise ValueError(f"tensor of {(batch,)} expected, not {tuple(t.shape)}")
     return _int32(t, 1)
 
 
 def burst_attn_cache_append(shp, cache, k, v, new_rows=None, rope=None, q=None, q_out=None, stream=None):
     """k, v [batch, sq, kv_heads, head_dim] bf16: sequence b's first new_rows[b] rows (all) become its rows rows[b] - new_rows[b] ..
     rows[b] - 1.  With a rotation the keys are turned, and q [batch, sq, q_heads, head_dim] into q_out."""
-    _check_device(k, v, q, q_out)
-    _check_cache(shp, cache)
-    _check_positions(shp, rope)
-    for t, heads in ((k, shp.kv_heads), (v, shp.kv_heads), (q, shp.q_heads), (q_out, shp.q_heads)):
-        _check_sizes(t, shp.batch, shp.sq, heads, shp.head_dim)
-    _check(_lib.burst_attn_cache_append(C.byref(shp), C.byref(cache), _ref(tensor(k)), _ref(tensor(v)), _numbers(new_rows, shp),
-                                        _ref(rope), _ref(tensor(q)), _ref(tensor(q_out)), _stream(stream)))
+    stream, device = _current(stream)
+    batch, sq, q_heads, kv_heads, d = shp.batch, shp.sq, shp.q_heads, shp.kv_heads, shp.head_dim
+    _check_cache(cache, batch, kv_heads, d)
+    _check_positions(rope, batch, sq)
+    _check(_lib.burst_attn_cache_append(shp, cache, _packed(k, device, batch, sq, kv_heads, d), _packed(v, device, batch, sq, kv_heads, d),
+                                        _numbers(new_rows, device, batch), rope, _packed(q, device, batch, sq, q_heads, d),
+                                        _packed(q_out, device, batch, sq, q_heads, d), stream))
 
 
 def burst_attn_decode_workspace_bytes(shp):
@@ -547,14 +565,17 @@ def burst_attn_decode_workspace_bytes(shp):
 def burst_attn_decode(shp, cache, q, o, lse=None, workspace=None, first_row=None, stream=None):
     """q [batch, 1, q_heads, head_dim] bf16 over the cache's rows from first_row[b] on: o (bf16 or fp32), lse [batch, q_heads, 1].
     shp.sk bounds the rows of a sequence; workspace: a one-byte tensor of burst_attn_decode_workspace_bytes(shp) bytes."""
-    _check_device(q, o, lse, workspace)
-    _check_cache(shp, cache)
-    _check_sizes(q, shp.batch, 1, shp.q_heads, shp.head_dim)
-    _check_sizes(o, shp.batch, 1, shp.q_heads, shp.head_dim)
-    _check_sizes(lse, shp.batch, shp.q_heads, 1)
+    stream, device = _current(stream)
+    batch, q_heads, kv_heads, d = shp.batch, shp.q_heads, shp.kv_heads, shp.head_dim
+    _check_cache(cache, batch, kv_heads, d)
+    _check_device(device, lse, workspace)
+    if lse is not None:
+        if lse.shape != (batch, q_heads, 1) or lse.dtype != torch.float32:
+            raise ValueError(f"lse: fp32 tensor of {(batch, q_heads, 1)} expected")
+        lse = _pack_rowvec(lse.data_ptr(), lse.stride(0), lse.stride(1))
     ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _check(_lib.burst_attn_decode(C.byref(shp), C.byref(cache), _ref(tensor(q)), _numbers(first_row, shp), _ref(tensor(o)),
-                                  _ref(rowvec(lse)), ws, n, _stream(stream)))
+    _check(_lib.burst_attn_decode(shp, cache, _packed(q, device, batch, 1, q_heads, d), _numbers(first_row, device, batch),
+                                  _packed(o, device, batch, 1, q_heads, d), lse, ws, n, stream))
 
 
 def burst_attn_mfma_probe(random_operands, iterations, stream=None):

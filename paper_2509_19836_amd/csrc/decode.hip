@@ -16,6 +16,7 @@
 //   work-groups as the chip holds at once, whatever the sequences' lengths are: each finds its first unit by a scan over
 //   the sequences.  A piece that is a whole (sequence, key head) is written out; what a work-group has of others goes to the workspace,
 //   two pieces at most, and decode_join_kernel adds the pieces up in a fixed order.
+#include <cstdlib>
 #include "cache.hpp"
 #include "kernels.hpp"
 #include "mfma16.hpp"
@@ -24,85 +25,95 @@ namespace burst {
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+// Read by scalar loads: a vector load of a page's number would have to be waited for together with all tiles asked for before it.
+typedef const __attribute__((address_space(4))) int32_t* scalar_table;
 
-constexpr int kWaves = 4, kTileRows = 32, kUnitRows = kWaves * kTileRows;
+constexpr int kTileRows = 32, kDealtWaves = 4;
+constexpr int kDirectWaves = 8;
 constexpr float kStale = 8.f;   // a maximum may fall behind by a factor of 2^8: P, O and their sums stay far inside fp32
 constexpr int kCus = 256;
-// Work-groups that share a CU, by the registers that a wave takes.
-constexpr int groups_per_cu(int head_dim, bool f8, int nc) { return nc == 2 ? 2 : head_dim == 64 ? 4 : f8 ? 3 : 2; }
+// Waves that share a SIMD, by the registers that one takes: work-groups of four waves that share a CU.
+constexpr int waves_per_simd(int head_dim, bool f8, int nc) { return nc == 2 ? 2 : 2 + (head_dim == 64) + f8; }
 
 // What a sequence's share of the work is.  It starts at a multiple of the tile, so that the halves of a tile lie in one page each where
 // pages are multiples of 16 rows; a sequence without rows has one unit, which writes its empty result.
 struct SeqRows {
   int32_t lo, hi, start, units;
 };
-__device__ __forceinline__ SeqRows seq_rows(const DecodeParams& p, int32_t n, int32_t first) {
+__device__ __forceinline__ SeqRows seq_rows(const DecodeParams& p, int32_t n, int32_t first, int unit_rows) {
   SeqRows s;
   const int32_t most = p.max_rows;   // (at most table_cols * page_rows, checked on the host)
   s.hi = n < 0 ? 0 : n > most ? most : n;
   s.lo = first < 0 ? 0 : first < s.hi ? first : s.hi;
   s.start = s.lo & ~(kTileRows - 1);
-  s.units = s.lo < s.hi ? (s.hi - s.start + kUnitRows - 1) / kUnitRows : 1;
+  s.units = s.lo < s.hi ? (s.hi - s.start + unit_rows - 1) / unit_rows : 1;
   return s;
 }
-__device__ __forceinline__ SeqRows seq_rows_of(const DecodeParams& p, int32_t b) {
-  return seq_rows(p, p.cache.rows[b], p.first_row ? p.first_row[b] : 0);
+__device__ __forceinline__ SeqRows seq_rows_of(const DecodeParams& p, int32_t b, int unit_rows) {
+  return seq_rows(p, p.cache.rows[b], p.first_row ? p.first_row[b] : 0, unit_rows);
 }
 
-// Units dealt to `groups` work-groups: the first `more` of them get one more.
+// Units dealt to `shares` work-groups: the first `more` of them get one more.
 struct Deal {
-  int64_t each, more;
-  __device__ __forceinline__ void init(int64_t units, int32_t groups) {
-    each = units >> 32 ? units / groups : (int64_t)((uint32_t)units / (uint32_t)groups);
-    more = units - each * groups;
+  int32_t each, more;
+  __device__ __forceinline__ void init(int32_t units, int32_t shares) {
+    each = __builtin_amdgcn_readfirstlane((int32_t)((uint32_t)units / (uint32_t)shares));
+    more = units - each * shares;
   }
-  __device__ __forceinline__ int64_t first(int32_t w) const { return w * each + (w < more ? w : more); }
-  __device__ __forceinline__ int32_t owner(int64_t unit) const {
-    const int64_t longer = more * (each + 1);
-    const int64_t x = unit < longer ? unit : unit - longer, y = unit < longer ? each + 1 : each;
-    const int64_t n = (x | y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
-    return (int32_t)(unit < longer ? n : more + n);
+  __device__ __forceinline__ int32_t first(int32_t w) const { return w * each + (w < more ? w : more); }
+  __device__ __forceinline__ int32_t owner(int32_t unit) const {
+    const int32_t longer = more * (each + 1);
+    return unit < longer ? (int32_t)((uint32_t)unit / (uint32_t)(each + 1)) : more + (int32_t)((uint32_t)(unit - longer) / (uint32_t)each);
   }
 };
 
-// The workspace: units of all, units before each sequence, and two pieces for every work-group, each (maximum, sum) and O of its
-// columns relative to that maximum.
+// Heads of a cache row that a work-group takes together, so that its waves read 256 bytes that lie side by side.
+constexpr int heads_side_by_side(int head_dim, bool f8) { return 256 / (head_dim * (f8 ? 1 : 2)); }
+
+// The workspace: for each sequence its first owner and, times two, its last one, plus one if the first owner's piece is its second (an owner is
+// a share of the units; every block of columns of every key head has the same shares); and two pieces for every work-group, each (maximum,
+// sum) and O of its columns relative to that maximum.
 struct DecodeSpace {
-  int64_t* units;
-  int64_t* before;
+  int2* owners;
   float2* ml;
   float* o;
   int32_t columns;   // of a piece: min(group, 16 NC)
 };
 
 struct DecodeShape {
-  int32_t blocks, groups;   // blocks of columns of a key head, work-groups
-  int32_t columns, max_units;
-  int64_t off_before, off_ml, off_o, bytes;
+  int32_t blocks, shares;   // blocks of columns of a key head; shares of a block's units, a work-group each
+  int32_t columns;
+  bool direct;              // a work-group for every (sequence, key head, block of columns), no workspace
+  int64_t off_ml, off_o, bytes;
 };
 static int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 static int columns_of(int32_t group) { return group <= 16 ? 16 : 32; }
-static DecodeShape decode_shape(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t max_rows, bool f8) {
+static DecodeShape decode_shape(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t max_rows, bool f8, int heads) {
   DecodeShape s;
   const int32_t group = q_heads / kv_heads, wide = columns_of(group);
   s.blocks = (group + wide - 1) / wide;
   s.columns = group < wide ? group : wide;
-  s.max_units = (int32_t)std::max<int64_t>(1, (max_rows + kUnitRows - 1) / kUnitRows);
-  const int64_t most = (int64_t)batch * kv_heads * s.blocks * s.max_units;
-  s.groups = (int32_t)std::min<int64_t>(most, kCus * groups_per_cu(head_dim, f8, wide / 16));
-  s.off_before = 256;
-  s.off_ml = s.off_before + up256((int64_t)batch * 8);
-  s.off_o = s.off_ml + up256((int64_t)s.groups * 2 * s.columns * 8);
-  s.bytes = s.max_units == 1 ? 0 : s.off_o + (int64_t)s.groups * 2 * s.columns * head_dim * 4;   // (a single unit is never shared)
+  const int64_t per_seq = (int64_t)kv_heads * s.blocks, unit = kTileRows * kDealtWaves / heads, max_units = (max_rows + unit - 1) / unit;
+  static const char* env = getenv("DIRECT_ROWS");
+  s.direct = max_rows <= (env ? atoi(env) : 1024);
+  const int64_t fit = std::max<int64_t>(1, kCus * waves_per_simd(head_dim, f8, wide / 16) * heads / per_seq);
+  s.shares = (int32_t)(s.direct ? batch : std::min<int64_t>(batch * max_units, fit));
+  const int64_t pieces = s.shares * per_seq * 2 * s.columns;
+  s.off_ml = up256((int64_t)batch * 8);
+  s.off_o = s.off_ml + up256(pieces * 8);
+  s.bytes = s.direct ? 0 : s.off_o + pieces * head_dim * 4;
   return s;
 }
 int64_t decode_workspace_bytes(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t max_rows) {
-  return std::max(decode_shape(batch, q_heads, kv_heads, head_dim, max_rows, false).bytes,
-                  decode_shape(batch, q_heads, kv_heads, head_dim, max_rows, true).bytes);
+  int64_t most = 0;
+  for (bool f8 : {false, true})
+    for (int heads : {1, heads_side_by_side(head_dim, f8)})
+      most = std::max(most, decode_shape(batch, q_heads, kv_heads, head_dim, max_rows, f8, heads).bytes);
+  return most;
 }
 static DecodeSpace space_of(const DecodeShape& s, void* workspace) {
   char* ws = (char*)workspace;
-  return DecodeSpace{(int64_t*)ws, (int64_t*)(ws + s.off_before), (float2*)(ws + s.off_ml), (float*)(ws + s.off_o), s.columns};
+  return DecodeSpace{(int2*)ws, (float2*)(ws + s.off_ml), (float*)(ws + s.off_o), s.columns};
 }
 
 // 8 numbers of e4m3 (two words) as a bf16 operand.
@@ -146,6 +157,13 @@ struct Tile {
   }
 };
 
+// A 32-bit offset that the compiler takes as new here: added to a scalar base it becomes an operand of the load, where one extended to 64
+// bits outside the loop would be added by the vector unit and take two registers.
+__device__ __forceinline__ uint32_t offset_here(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Where a tile's rows lie, and which of them are seen (a bit for each).
 struct TilePlace {
   uint32_t seen;
@@ -154,88 +172,117 @@ struct TilePlace {
   int64_t row;             // any pages: bytes to this lane's row (lane % 32)
 };
 
-template <int D, bool F8, int NC, bool PAGES16>
-__global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(DecodeParams p, DecodeSpace ws, int32_t blocks, int32_t groups) {
-  constexpr int KK = D / 32, DT = D / 16, kBytes = F8 ? 1 : 2;
+// The sequence that holds the first unit of a work-group, found by a scan over all.
+struct FirstUnit {
+  SeqRows seq;
+  int32_t b, at;   // the sequence, and which of its units
+};
+
+template <int D, bool F8, int NC, bool PAGES16, bool DIRECT, int HEADS>
+__global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, waves_per_simd(D, F8, NC)) void decode_kernel(DecodeParams p, DecodeSpace ws,
+                                                                                                         int32_t blocks, int32_t shares) {
+  constexpr int KK = D / 32, DT = D / 16, kBytes = F8 ? 1 : 2, kWaves = DIRECT ? kDirectWaves : kDealtWaves, kRowWaves = kWaves / HEADS, kUnit = kRowWaves * kTileRows;
   __shared__ float part_o[kWaves][16][D + 4];
   __shared__ float2 part_ml[kWaves][NC * 16];
-  __shared__ int64_t scan[kWaves + 2];
+  constexpr bool kQInLds = NC == 2;   // two blocks of 16 queries do not fit in the registers beside their sums
+  __shared__ bf16x8 q_lds[kQInLds ? HEADS : 1][kQInLds ? NC * KK : 1][64];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int32_t group = p.q_heads / p.kv_heads, per_seq = p.kv_heads * blocks;
+  const int head_wave = wave % HEADS, row_wave = wave / HEADS;
 
-  // All units, and the sequence that holds this work-group's first one.
-  int64_t total = 0;
-  int32_t mine = 0;
-  for (int32_t b0 = 0; b0 < p.batch; b0 += 256) {
-    mine = b0 + tid < p.batch ? seq_rows_of(p, b0 + tid).units : 0;
-    int32_t sum = mine;   // (at most 2^23 units a sequence, 64 of them)
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-    if (lane == 0) scan[wave] = sum;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) total += scan[w];
-    __syncthreads();
-  }
+  // Heads next to each other are work-groups next to each other: their rows lie side by side in most caches, and are read at the same time.
+  const int32_t share = (int32_t)blockIdx.x / (per_seq / HEADS), hb = (int32_t)blockIdx.x - share * (per_seq / HEADS);
+  const int32_t hk0 = hb / blocks * HEADS, cb = hb % blocks, c0 = cb * 16 * NC;   // the first head; first of the block's columns in a group
+  const int32_t hk = hk0 + head_wave;                                           // this wave's head
+
+  SeqRows seq;
+  int32_t b, at = 0;
+  int32_t unit = 0, left = 1;
   Deal deal;
-  deal.init(total * per_seq, groups);
-  int64_t unit = deal.first(blockIdx.x), left = deal.first(blockIdx.x + 1) - unit;
-  if (left == 0) return;
-  int64_t passed = 0;
-  for (int32_t b0 = 0; b0 < p.batch; b0 += 256) {
-    if (p.batch > 256) mine = b0 + tid < p.batch ? seq_rows_of(p, b0 + tid).units : 0;
-    int32_t upto = mine;
+  if constexpr (DIRECT) {
+    b = share;
+    seq = seq_rows_of(p, b, kUnit);
+  } else {
+    __shared__ int32_t scan[kWaves];
+    __shared__ FirstUnit found;
+    int32_t total = 0;   // (below 2^31, checked on the host)
+    SeqRows mine = {};
+    for (int32_t b0 = 0; b0 < p.batch; b0 += 256) {
+      mine = b0 + tid < p.batch ? seq_rows_of(p, b0 + tid, kUnit) : SeqRows{};
+      int32_t sum = mine.units;
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const int32_t y = __shfl_up(upto, x, 64);
-      upto += lane >= x ? y : 0;
+      for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
+      if (lane == 0) scan[wave] = sum;
+      __syncthreads();
+      for (int w = 0; w < kWaves; ++w) total += scan[w];
+      __syncthreads();
     }
-    if (lane == 63) scan[wave] = upto;
-    __syncthreads();
-    int64_t before = passed;
-    for (int w = 0; w < kWaves; ++w) {
-      before += w < wave ? scan[w] : 0;
-      passed += scan[w];
+    deal.init(__builtin_amdgcn_readfirstlane(total), shares);
+    unit = deal.first(share);
+    left = deal.first(share + 1) - unit;
+    if (left == 0) return;
+    int32_t passed = 0;
+    for (int32_t b0 = 0; b0 < p.batch; b0 += 256) {
+      if (p.batch > 256) mine = b0 + tid < p.batch ? seq_rows_of(p, b0 + tid, kUnit) : SeqRows{};
+      int32_t upto = mine.units;
+#pragma unroll
+      for (int x = 1; x < 64; x <<= 1) {
+        const int32_t y = __shfl_up(upto, x, 64);
+        upto += lane >= x ? y : 0;
+      }
+      if (lane == 63) scan[wave] = upto;
+      __syncthreads();
+      int32_t begin = passed + upto - mine.units;
+      for (int w = 0; w < kWaves; ++w) {
+        begin += w < wave ? scan[w] : 0;
+        passed += scan[w];
+      }
+      if (begin <= unit && unit < begin + mine.units) found = FirstUnit{mine, b0 + tid, unit - begin};   // (one thread)
+      __syncthreads();
+      if (passed > unit) break;
     }
-    const int64_t end = before + upto, begin = end - mine;
-    if (begin * per_seq <= unit && unit < end * per_seq) {   // (one thread: a sequence without units is none of the batch)
-      scan[kWaves] = begin;
-      scan[kWaves + 1] = b0 + tid;
-    }
-    __syncthreads();
-    if (passed * per_seq > unit) break;
+    b = __builtin_amdgcn_readfirstlane(found.b);
+    seq.lo = __builtin_amdgcn_readfirstlane(found.seq.lo);
+    seq.hi = __builtin_amdgcn_readfirstlane(found.seq.hi);
+    seq.start = __builtin_amdgcn_readfirstlane(found.seq.start);
+    seq.units = __builtin_amdgcn_readfirstlane(found.seq.units);
+    at = __builtin_amdgcn_readfirstlane(found.at);
   }
-  int64_t before = scan[kWaves];
-  int32_t b = __builtin_amdgcn_readfirstlane((int32_t)scan[kWaves + 1]);
-  if (ws.units && blockIdx.x == 0 && tid == 0) *ws.units = total;
-
-  SeqRows seq = seq_rows_of(p, b);
-  int64_t in_seq = unit - before * per_seq;
-  int32_t hb = __builtin_amdgcn_readfirstlane((int32_t)(in_seq / seq.units));
-  int32_t at = __builtin_amdgcn_readfirstlane((int32_t)(in_seq - (int64_t)hb * seq.units));
 
   const uint32_t row_bytes = (uint32_t)p.cache.s_row * kBytes;
   const uint32_t k_lane = r * row_bytes + 16 * g, v_lane = 4 * g * row_bytes + DT * kBytes * r;
   bool first_piece = true;
 
   while (left > 0) {
-    const int32_t take = (int32_t)(left < seq.units - at ? left : seq.units - at);
-    const int32_t hk = hb / blocks, c0 = (hb - hk * blocks) * 16 * NC;   // first of the block's columns in its group
-    const bool whole = at == 0 && take == seq.units;
-    if (ws.units && hb == 0 && at == 0 && tid == 0) ws.before[b] = before;
-
-    bf16x8 q[NC][KK];
-#pragma unroll
-    for (int nc = 0; nc < NC; ++nc) {
-      const int32_t c = c0 + 16 * nc + r;
-      const __bf16* row = (const __bf16*)p.q.ptr + b * p.q.sb + (int64_t)(hk * group + c) * p.q.sh;
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
-        q[nc][kk] = c < group ? *reinterpret_cast<const bf16x8*>(row + Tile<D, F8>::q_element(g, kk)) : bf16x8{};
+    const int32_t take = DIRECT ? seq.units : left < seq.units - at ? left : seq.units - at;
+    const bool whole = DIRECT || (at == 0 && take == seq.units);
+    if constexpr (!DIRECT) {
+      if (hb == 0 && at == 0 && tid == 0) {
+        const int32_t last = whole ? share : deal.owner(unit + seq.units - 1);
+        ws.owners[b] = int2{share, 2 * last + (first_piece ? 0 : 1)};
+      }
     }
+
+    bf16x8 q[kQInLds ? 1 : NC][KK];
+    if (!kQInLds || row_wave == 0) {
+#pragma unroll
+      for (int nc = 0; nc < NC; ++nc) {
+        const int32_t c = c0 + 16 * nc + r;
+        const __bf16* row = (const __bf16*)p.q.ptr + b * p.q.sb + (int64_t)(hk * group + c) * p.q.sh;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          const bf16x8 x = c < group ? *reinterpret_cast<const bf16x8*>(row + Tile<D, F8>::q_element(g, kk)) : bf16x8{};
+          if constexpr (kQInLds) q_lds[head_wave][nc * KK + kk][lane] = x;
+          else q[nc][kk] = x;
+        }
+      }
+    }
+    if constexpr (kQInLds) __syncthreads();
     const float to_log2 = p.scale * kLog2e * (F8 && p.cache.k_scale ? p.cache.k_scale[hk] : 1.f);
     const char* k_base = (const char*)p.cache.k + hk * p.cache.s_head * kBytes;
     const char* v_base = (const char*)p.cache.v + hk * p.cache.s_head * kBytes;
     const int32_t* table = p.cache.table + b * p.cache.table_stride;
+    const scalar_table pages = (scalar_table)table;
 
     float m[NC], l[NC];
     f32x4 acc[NC][DT];
@@ -247,14 +294,20 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
       for (int j = 0; j < DT; ++j) acc[nc][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // this wave's tiles: every fourth from t0 on, below t1
-    const int32_t t1 = seq.units == at + take ? seq.hi : seq.start + (at + take) * kUnitRows;
-    int32_t t = seq.start + at * kUnitRows + wave * kTileRows;
+    // this wave's tiles: from t on every kRowWaves-th one, below t1
+    const int32_t t1 = seq.units == at + take ? seq.hi : seq.start + (at + take) * kUnit;
+    int32_t t = seq.start + at * kUnit + row_wave * kTileRows;
 
-    auto page_of = [&](int32_t row) -> int32_t {   // (the whole wave's row)
-      if (row >= seq.hi) return -1;
-      const int32_t page = table[p.cache.by_page.quotient(row)];
-      return __builtin_amdgcn_readfirstlane(page >= 0 && page < p.cache.n_pages ? page : -1);
+    // The pages of a tile as the table says them: of its two halves, or of this lane's row (lane % 32).  Asked for up to the bound, not the
+    // sequence's end, so that the first look-up does not wait for that.
+    auto look_up = [&](int32_t row0, int32_t (&page)[2]) {
+      if constexpr (PAGES16) {
+        page[0] = row0 < p.max_rows ? pages[p.cache.by_page.quotient(row0)] : -1;
+        page[1] = row0 + 16 < p.max_rows ? pages[p.cache.by_page.quotient(row0 + 16)] : -1;
+      } else {
+        const int32_t row = row0 + (lane & 31);
+        page[0] = row < p.max_rows ? table[p.cache.by_page.quotient(row)] : -1;
+      }
     };
     auto place = [&](int32_t row0, const int32_t (&page)[2], TilePlace& x) {
       // rows of the tile that the sequence has
@@ -265,8 +318,9 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           int64_t off = 0;   // a half without a page: any rows that are there, unseen
-          if (page[h] >= 0) {
-            const int32_t row = row0 + 16 * h, in_page = row - p.cache.by_page.quotient(row) * p.cache.page_rows;
+          const int32_t row = row0 + 16 * h;
+          if (row < seq.hi && page[h] >= 0 && page[h] < p.cache.n_pages) {
+            const int32_t in_page = row - p.cache.by_page.quotient(row) * p.cache.page_rows;
             off = (page[h] * p.cache.s_page + in_page * p.cache.s_row) * kBytes;
           } else {
             seen &= h ? 0x0000ffffu : 0xffff0000u;
@@ -276,63 +330,61 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
         }
         x.seen = seen;
       } else {
-        const int32_t row = row0 + (lane & 31);
-        int64_t off = -1;
-        if (row < seq.hi) off = p.cache.row_offset(b, row);
-        x.seen = seen & (uint32_t)__ballot(off >= 0);
-        x.row = off >= 0 ? off * kBytes : 0;
+        const int32_t row = row0 + (lane & 31), in_page = row - p.cache.by_page.quotient(row) * p.cache.page_rows;
+        const bool there = row < seq.hi && page[0] >= 0 && page[0] < p.cache.n_pages;
+        x.seen = seen & (uint32_t)__ballot(there);
+        x.row = there ? (page[0] * p.cache.s_page + in_page * p.cache.s_row) * kBytes : 0;
       }
     };
     Tile<D, F8> tile;
     auto load_k = [&](const TilePlace& x) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if constexpr (PAGES16) tile.load_k(h, x.half_k[h] + k_lane);
+        if constexpr (PAGES16) tile.load_k(h, x.half_k[h] + offset_here(k_lane));
         else tile.load_k(h, k_base + __shfl(x.row, 16 * h + r, 64) + 16 * g);
       }
     };
     auto load_v = [&](const TilePlace& x) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (PAGES16) tile.load_v(e, x.half_v[e >> 2] + (v_lane + (e & 3) * row_bytes));
+        if constexpr (PAGES16) tile.load_v(e, x.half_v[e >> 2] + offset_here(v_lane + (e & 3) * row_bytes));
         else tile.load_v(e, v_base + __shfl(x.row, 16 * (e >> 2) + 4 * g + (e & 3), 64) + DT * kBytes * r);
       }
     };
 
     int32_t page[2] = {-1, -1};
     TilePlace now;
+    look_up(t, page);
     if (t < t1) {
-      if constexpr (PAGES16) {
-        page[0] = page_of(t);
-        page[1] = page_of(t + 16);
-      }
       place(t, page, now);
       load_k(now);
       load_v(now);
-      if constexpr (PAGES16) {
-        page[0] = page_of(t + kUnitRows);
-        page[1] = page_of(t + kUnitRows + 16);
-      }
+      look_up(t + kUnit, page);
     }
-    for (; t < t1; t += kUnitRows) {
-      const bool more = t + kUnitRows < t1;
+    for (; t < t1; t += kUnit) {
+      // (pages of any size: behind the last tile row 0 of page 0 is asked for, by all lanes; with a condition there the compiler forgets registers
+      // that are still to be read, which the build refuses)
+      const bool more = !PAGES16 || t + kUnit < t1;
       f32x4 s[NC][2];
+      if constexpr (kQInLds) asm volatile("" ::: "memory");   // (or the compiler reads the queries once, into registers)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
           const bf16x8 a = tile.k_operand(h, kk);
 #pragma unroll
-          for (int nc = 0; nc < NC; ++nc) s[nc][h] = mfma16(a, q[nc][kk], kk == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[nc][h]);
+          for (int nc = 0; nc < NC; ++nc) {
+            bf16x8 qv;
+            if constexpr (kQInLds) qv = q_lds[head_wave][nc * KK + kk][lane];
+            else qv = q[nc][kk];
+            s[nc][h] = mfma16(a, qv, kk == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[nc][h]);
+          }
         }
       const uint32_t seen = now.seen;
       if (more) {
-        place(t + kUnitRows, page, now);
+        place(t + kUnit, page, now);
         load_k(now);
-        if constexpr (PAGES16) {
-          page[0] = page_of(t + 2 * kUnitRows);
-          page[1] = page_of(t + 2 * kUnitRows + 16);
-        }
+        look_up(t + 2 * kUnit, page);
       }
       // this lane's keys: bit 16 (e / 4) + 4g + e % 4
       const uint32_t bits = ((seen >> (4 * g)) & 15u) | ((seen >> (4 * g + 12)) & 0xf0u);
@@ -410,7 +462,7 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
       if (more) load_v(now);
     }
 
-    // The four waves' sums against their largest maximum.  Lane (r, g) has of column r the elements DT (4g + v) + j.
+    // The waves' sums against their largest maximum.  Lane (r, g) has of column r the elements DT (4g + v) + j.
 #pragma unroll
     for (int nc = 0; nc < NC; ++nc) {
       l[nc] += __shfl_xor(l[nc], 16, 64);
@@ -422,7 +474,7 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
     for (int nc = 0; nc < NC; ++nc) {
       float top = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, part_ml[w][16 * nc + r].x);
+      for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, part_ml[w * HEADS + head_wave][16 * nc + r].x);
       const float f = m[nc] == top ? 1.f : __builtin_amdgcn_exp2f(m[nc] - top);
 #pragma unroll
       for (int v = 0; v < 4; ++v)
@@ -431,63 +483,58 @@ __global__ __launch_bounds__(256, groups_per_cu(D, F8, NC)) void decode_kernel(D
           *reinterpret_cast<f32x4*>(&part_o[wave][r][DT * (4 * g + v) + j]) =
               f32x4{acc[nc][j][v] * f, acc[nc][j + 1][v] * f, acc[nc][j + 2][v] * f, acc[nc][j + 3][v] * f};
       __syncthreads();
-      for (int i = tid; i < 16 * (D / 4); i += 256) {
-        const int c = i / (D / 4), d = i % (D / 4) * 4, column = c0 + 16 * nc + c;
+      for (int i = tid; i < HEADS * 16 * (D / 4); i += 64 * kWaves) {
+        const int hw = i / (16 * (D / 4)), c = i / (D / 4) % 16, d = i % (D / 4) * 4, column = c0 + 16 * nc + c, head = hk0 + hw;
         if (column >= group) continue;
         float most = -INFINITY, sum = 0.f;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, part_ml[w][16 * nc + c].x);
+        for (int w = 0; w < kRowWaves; ++w) most = fmaxf(most, part_ml[w * HEADS + hw][16 * nc + c].x);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const float2 ml = part_ml[w][16 * nc + c];
+        for (int w = 0; w < kRowWaves; ++w) {
+          const float2 ml = part_ml[w * HEADS + hw][16 * nc + c];
           sum += ml.y * (ml.x == most ? 1.f : __builtin_amdgcn_exp2f(ml.x - most));
-          o += *reinterpret_cast<const f32x4*>(&part_o[w][c][d]);
+          o += *reinterpret_cast<const f32x4*>(&part_o[w * HEADS + hw][c][d]);
         }
         if (whole) {
-          const int32_t h = hk * group + column;
-          const float over = sum == 0.f ? 0.f : (F8 && p.cache.v_scale ? p.cache.v_scale[hk] : 1.f) / sum;
+          const int32_t h = head * group + column;
+          const float over = sum == 0.f ? 0.f : (F8 && p.cache.v_scale ? p.cache.v_scale[head] : 1.f) / sum;
           const int64_t to = b * p.o.sb + h * p.o.sh + d;
           o *= over;
           if (p.o.is_f32) *reinterpret_cast<f32x4*>((float*)p.o.ptr + to) = o;
           else *reinterpret_cast<bf16x4*>((__bf16*)p.o.ptr + to) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
           if (d == 0 && p.lse.ptr) p.lse.ptr[b * p.lse.sb + h * p.lse.sh] = sum == 0.f ? -INFINITY : (most + __log2f(sum)) * kLn2;
         } else {
-          const int64_t piece = (int64_t)(2 * blockIdx.x + (first_piece ? 0 : 1)) * ws.columns + 16 * nc + c;
+          const int64_t piece = (2 * ((int64_t)share * per_seq + head * blocks + cb) + (first_piece ? 0 : 1)) * ws.columns + 16 * nc + c;
           *reinterpret_cast<f32x4*>(ws.o + piece * D + d) = o;
           if (d == 0) ws.ml[piece] = float2{most, sum};
         }
       }
       __syncthreads();
     }
+    if constexpr (DIRECT) break;
     first_piece = false;
+    unit += take;
     left -= take;
     at = 0;
-    if (left > 0 && ++hb == per_seq) {
-      hb = 0;
-      before += seq.units;
-      seq = seq_rows_of(p, ++b);
-    }
+    if (left > 0) seq = seq_rows_of(p, ++b, kUnit);
   }
 }
 
 // A (sequence, query head) whose rows several work-groups had: their pieces added up.
 template <int D, int NC>
-__global__ __launch_bounds__(256) void decode_join_kernel(DecodeParams p, DecodeSpace ws, int32_t blocks, int32_t groups, int32_t f8) {
+__global__ __launch_bounds__(256) void decode_join_kernel(DecodeParams p, DecodeSpace ws, int32_t blocks) {
   constexpr int LANES = D / 4, ROWS = 256 / LANES;
   __shared__ float top_w[4];
   __shared__ f32x4 part[ROWS][LANES];
   __shared__ float sums[ROWS];
-  const int32_t b = blockIdx.x / p.q_heads, h = blockIdx.x - b * p.q_heads, group = p.q_heads / p.kv_heads;
+  const int32_t b = (int32_t)blockIdx.x / p.q_heads, h = (int32_t)blockIdx.x - b * p.q_heads, group = p.q_heads / p.kv_heads;
   const int32_t hk = h / group, column = h - hk * group, cb = column / (16 * NC), c = column - cb * 16 * NC;
-  const int32_t per_seq = p.kv_heads * blocks, units = seq_rows_of(p, b).units;
-  Deal deal;
-  deal.init(*ws.units * per_seq, groups);
-  const int64_t unit = ws.before[b] * per_seq + (int64_t)(hk * blocks + cb) * units;
-  const int32_t w0 = deal.owner(unit), w1 = deal.owner(unit + units - 1);
+  const int2 owners = ws.owners[b];
+  const int32_t w0 = owners.x, w1 = owners.y >> 1, skip = owners.y & 1;
   if (w0 == w1) return;   // written out by its only owner
-  const int32_t skip = deal.first(w0) < unit ? 1 : 0;   // the first owner has something else before it
-  auto piece = [&](int32_t w) { return (int64_t)(2 * w + (w == w0 ? skip : 0)) * ws.columns + c; };
+  const int32_t per_seq = p.kv_heads * blocks, hb = hk * blocks + cb;
+  auto piece = [&](int32_t w) { return (2 * ((int64_t)w * per_seq + hb) + (w == w0 ? skip : 0)) * ws.columns + c; };
   float top = -INFINITY;
   for (int32_t w = w0 + threadIdx.x; w <= w1; w += 256) top = fmaxf(top, ws.ml[piece(w)].x);
 #pragma unroll
@@ -512,38 +559,46 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeParams p, Decode
     o += part[i][lane];
     sum += sums[i];
   }
-  o *= sum == 0.f ? 0.f : (f8 && p.cache.v_scale ? p.cache.v_scale[hk] : 1.f) / sum;
+  o *= sum == 0.f ? 0.f : (p.cache.v_scale ? p.cache.v_scale[hk] : 1.f) / sum;
   const int64_t to = b * p.o.sb + h * p.o.sh + 4 * lane;
   if (p.o.is_f32) *reinterpret_cast<f32x4*>((float*)p.o.ptr + to) = o;
   else *reinterpret_cast<bf16x4*>((__bf16*)p.o.ptr + to) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
   if (lane == 0 && p.lse.ptr) p.lse.ptr[b * p.lse.sb + h * p.lse.sh] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
 }
 
-template <int D, int NC>
+template <int D, bool F8, int NC, bool PAGES16>
 static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
-  const DecodeShape s = decode_shape(p.batch, p.q_heads, p.kv_heads, D, p.max_rows, p.cache.is_f8 != 0);
-  DecodeSpace ws = {};
-  if (s.bytes > 0) ws = space_of(s, p.workspace);
-  const dim3 grid(s.groups), block(256);
-  const bool pages16 = p.cache.page_rows % 16 == 0;
-  if (p.cache.is_f8) {
-    if (pages16) hipLaunchKernelGGL((decode_kernel<D, true, NC, true>), grid, block, 0, stream, p, ws, s.blocks, s.groups);
-    else hipLaunchKernelGGL((decode_kernel<D, true, NC, false>), grid, block, 0, stream, p, ws, s.blocks, s.groups);
-  } else {
-    if (pages16) hipLaunchKernelGGL((decode_kernel<D, false, NC, true>), grid, block, 0, stream, p, ws, s.blocks, s.groups);
-    else hipLaunchKernelGGL((decode_kernel<D, false, NC, false>), grid, block, 0, stream, p, ws, s.blocks, s.groups);
+  constexpr int kSide = heads_side_by_side(D, F8);
+  const int heads = p.kv_heads % kSide == 0 && p.cache.s_head == D ? kSide : 1;
+  const DecodeShape s = decode_shape(p.batch, p.q_heads, p.kv_heads, D, p.max_rows, F8, heads);
+  const dim3 grid((uint32_t)((int64_t)s.shares * p.kv_heads * s.blocks / (s.direct ? 1 : heads)));
+  if (s.direct) {
+    hipLaunchKernelGGL((decode_kernel<D, F8, NC, PAGES16, true, 1>), grid, dim3(64 * kDirectWaves), 0, stream, p, DecodeSpace{}, s.blocks, s.shares);
+    return hipGetLastError();
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || s.max_units == 1) return e;
-  hipLaunchKernelGGL((decode_join_kernel<D, NC>), dim3((uint32_t)(p.batch * p.q_heads)), block, 0, stream, p, ws, s.blocks, s.groups,
-                     p.cache.is_f8);
+  const DecodeSpace ws = space_of(s, p.workspace);
+  if (heads > 1) hipLaunchKernelGGL((decode_kernel<D, F8, NC, PAGES16, false, kSide>), grid, dim3(64 * kDealtWaves), 0, stream, p, ws, s.blocks, s.shares);
+  else hipLaunchKernelGGL((decode_kernel<D, F8, NC, PAGES16, false, 1>), grid, dim3(64 * kDealtWaves), 0, stream, p, ws, s.blocks, s.shares);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((decode_join_kernel<D, NC>), dim3((uint32_t)(p.batch * p.q_heads)), dim3(256), 0, stream, p, ws, s.blocks);
   return hipGetLastError();
 }
 
-hipError_t launch_decode(const DecodeParams& p, hipStream_t stream) {
+template <int D, bool F8>
+static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   const bool wide = columns_of(p.q_heads / p.kv_heads) == 32;
-  if (p.head_dim == 128) return wide ? launch<128, 2>(p, stream) : launch<128, 1>(p, stream);
-  return wide ? launch<64, 2>(p, stream) : launch<64, 1>(p, stream);
+  if (p.cache.page_rows % 16 == 0) return wide ? launch<D, F8, 2, true>(p, stream) : launch<D, F8, 1, true>(p, stream);
+  return wide ? launch<D, F8, 2, false>(p, stream) : launch<D, F8, 1, false>(p, stream);
+}
+
+template <int D>
+static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
+  return p.cache.is_f8 ? launch<D, true>(p, stream) : launch<D, false>(p, stream);
+}
+
+hipError_t launch_decode(const DecodeParams& p, hipStream_t stream) {
+  return p.head_dim == 128 ? launch<128>(p, stream) : launch<64>(p, stream);
 }
 
 }  // namespace burst

@@ -38,7 +38,8 @@ class Calls:
         return copy
 
     def ref(self, x):
-        return None if x is None else C.byref(x)
+        """Structs by reference; tensors and row vectors, which these calls take as bytes, as those."""
+        return None if x is None else bytes(x) if isinstance(x, (self.lib.burst_tensor_t, self.lib.burst_rowvec_t)) else C.byref(x)
 
     def turn(self, **kw):
         a = dict(shape=self.shape(), rope=self.rope, q=self.t, q_out=self.tensor(0x20000), k=self.tensor(0x30000), k_out=self.tensor(0x40000))
@@ -159,7 +160,8 @@ def test_tensors_of_the_wrong_kind_are_refused_by_the_binding(lib, monkeypatch):
         lib.rope(torch.zeros(1, 1, 4, dtype=torch.int32), torch.zeros(32))
     with pytest.raises(ValueError, match="current device"):
         lib.paged_cache(cpu, cpu, torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
-    monkeypatch.setattr(lib, "_check_device", lambda *t: None)
+    monkeypatch.setattr(lib, "_current", lambda stream: (None, -1))                  # as if the CPU were the current device
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
     with pytest.raises(ValueError, match="axis_of_pair"):
         lib.rope(torch.zeros(1, 1, 4, dtype=torch.int32), torch.zeros(32), axis_of_pair=[1] * 32)
     with pytest.raises(ValueError, match="int32"):
@@ -175,9 +177,13 @@ def test_tensors_of_the_wrong_kind_are_refused_by_the_binding(lib, monkeypatch):
     cache = lib.paged_cache(pages, pages, torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
     with pytest.raises(ValueError, match="another batch"):
         lib.burst_attn_decode(lib.shape(2, 2, 2, 64, 1, 16, 1.0), cache, cpu, cpu)
-    for empty in (cpu[:0],):
-        with pytest.raises(ValueError):
-            lib.burst_attn_rope(lib.shape(1, 2, 2, 64, 4, 0, 1.0), r, cpu, empty)
+    with pytest.raises(ValueError, match="tensor of"):
+        lib.burst_attn_rope(lib.shape(1, 2, 2, 64, 4, 0, 1.0), r, cpu, cpu[:0])
+    with pytest.raises(ValueError, match="contiguous"):
+        lib.burst_attn_rope(lib.shape(1, 2, 2, 64, 4, 0, 1.0), r, cpu, torch.zeros(1, 4, 64, 2).transpose(2, 3))
+    with pytest.raises(ValueError, match="lse"):
+        q = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16)
+        lib.burst_attn_decode(lib.shape(1, 2, 2, 64, 1, 16, 1.0), cache, q, q, lse=torch.zeros(1, 2, 2))
 
 
 def test_quotients_by_the_page_size(lib):
