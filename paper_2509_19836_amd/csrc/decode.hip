@@ -16,7 +16,6 @@
 //   work-groups as the chip holds at once, whatever the sequences' lengths are: each finds its first unit by a scan over
 //   the sequences.  A piece that is a whole (sequence, key head) is written out; what a work-group has of others goes to the workspace,
 //   two pieces at most, and decode_join_kernel adds the pieces up in a fixed order.
-#include <cstdlib>
 #include "cache.hpp"
 #include "kernels.hpp"
 #include "mfma16.hpp"
@@ -67,8 +66,8 @@ struct Deal {
   }
 };
 
-// Heads of a cache row that a work-group takes together, so that its waves read 256 bytes that lie side by side.
-constexpr int heads_side_by_side(int head_dim, bool f8) { return 256 / (head_dim * (f8 ? 1 : 2)); }
+// Heads of a cache row that the waves of a work-group take beside each other, 512 bytes where they lie side by side.
+constexpr int heads_side_by_side(int head_dim, bool f8) { return head_dim == 128 && !f8 ? 2 : 4; }
 
 // The workspace: for each sequence its first owner and, times two, its last one, plus one if the first owner's piece is its second (an owner is
 // a share of the units; every block of columns of every key head has the same shares); and two pieces for every work-group, each (maximum,
@@ -94,8 +93,9 @@ static DecodeShape decode_shape(int32_t batch, int32_t q_heads, int32_t kv_heads
   s.blocks = (group + wide - 1) / wide;
   s.columns = group < wide ? group : wide;
   const int64_t per_seq = (int64_t)kv_heads * s.blocks, unit = kTileRows * kDealtWaves / heads, max_units = (max_rows + unit - 1) / unit;
-  static const char* env = getenv("DIRECT_ROWS");
-  s.direct = max_rows <= (env ? atoi(env) : 1024);
+  // The line between the two: a work-group for each (sequence, key head) saves the scan and the second kernel and reads its rows by itself.
+  const int64_t head_bytes = max_rows * head_dim * (f8 ? 2 : 4);
+  s.direct = head_bytes <= (batch * per_seq < kCus ? 256 << 10 : 512 << 10);
   const int64_t fit = std::max<int64_t>(1, kCus * waves_per_simd(head_dim, f8, wide / 16) * heads / per_seq);
   s.shares = (int32_t)(s.direct ? batch : std::min<int64_t>(batch * max_units, fit));
   const int64_t pieces = s.shares * per_seq * 2 * s.columns;
@@ -124,7 +124,14 @@ __device__ __forceinline__ bf16x8 widened(uint32_t w0, uint32_t w1) {
 }
 
 // A tile's keys and values in a wave's registers.
-template <int D, bool F8>
+// NT: the cache is larger than what stays on the chip from one call to the next: its lines are not kept (read-through, see launch).
+template <class T, bool NT>
+__device__ __forceinline__ T read_once(const char* at) {
+  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const T*>(at));
+  else return *reinterpret_cast<const T*>(at);
+}
+
+template <int D, bool F8, bool NT>
 struct Tile {
   static constexpr int kBytes = F8 ? 1 : 2;
   static constexpr int KW = D * kBytes / 64;         // 16-byte pieces of a K row in a lane
@@ -140,19 +147,19 @@ struct Tile {
   __device__ __forceinline__ static int q_element(int g, int kk) { return F8 ? 64 * (kk / 2) + 16 * g + 8 * (kk & 1) : 32 * kk + 8 * g; }
   __device__ __forceinline__ void load_k(int t, const char* row) {   // of this lane: row 16 t + r, its piece g
 #pragma unroll
-    for (int i = 0; i < KW; ++i) k[t][i] = *reinterpret_cast<const u32x4*>(row + 64 * i);
+    for (int i = 0; i < KW; ++i) k[t][i] = read_once<u32x4, NT>(row + 64 * i);
   }
   __device__ __forceinline__ void load_v(int e, const char* row) {   // of this lane: key e, elements D / 16 r ..
     if constexpr (VW == 4) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(row);
+      const u32x4 x = read_once<u32x4, NT>(row);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[e][i] = x[i];
     } else if constexpr (VW == 2) {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(row);
+      const u32x2 x = read_once<u32x2, NT>(row);
       v[e][0] = x[0];
       v[e][1] = x[1];
     } else {
-      v[e][0] = *reinterpret_cast<const uint32_t*>(row);
+      v[e][0] = read_once<uint32_t, NT>(row);
     }
   }
 };
@@ -271,7 +278,7 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
         const __bf16* row = (const __bf16*)p.q.ptr + b * p.q.sb + (int64_t)(hk * group + c) * p.q.sh;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-          const bf16x8 x = c < group ? *reinterpret_cast<const bf16x8*>(row + Tile<D, F8>::q_element(g, kk)) : bf16x8{};
+          const bf16x8 x = c < group ? *reinterpret_cast<const bf16x8*>(row + Tile<D, F8, !DIRECT>::q_element(g, kk)) : bf16x8{};
           if constexpr (kQInLds) q_lds[head_wave][nc * KK + kk][lane] = x;
           else q[nc][kk] = x;
         }
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
         x.row = there ? (page[0] * p.cache.s_page + in_page * p.cache.s_row) * kBytes : 0;
       }
     };
-    Tile<D, F8> tile;
+    Tile<D, F8, !DIRECT> tile;
     auto load_k = [&](const TilePlace& x) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -431,7 +438,7 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-          for (int i = 0; i < Tile<D, F8>::VW; ++i) tile.v[e][i] = (bits >> e) & 1u ? tile.v[e][i] : 0u;
+          for (int i = 0; i < Tile<D, F8, !DIRECT>::VW; ++i) tile.v[e][i] = (bits >> e) & 1u ? tile.v[e][i] : 0u;
       }
       uint32_t v2[8][DT / 2];   // as bf16: words of two elements
 #pragma unroll
@@ -535,21 +542,37 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeParams p, Decode
   if (w0 == w1) return;   // written out by its only owner
   const int32_t per_seq = p.kv_heads * blocks, hb = hk * blocks + cb;
   auto piece = [&](int32_t w) { return (2 * ((int64_t)w * per_seq + hb) + (w == w0 ? skip : 0)) * ws.columns + c; };
+  const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
+  constexpr int U = 8;   // pieces under way for a thread; the first ones while the largest maximum is looked for
+  f32x4 x[U];
+  float2 ml[U];
+  auto load = [&](int32_t w) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = piece(w + u * ROWS < w1 ? w + u * ROWS : w1);
+      x[u] = *reinterpret_cast<const f32x4*>(ws.o + at * D + 4 * lane);
+      ml[u] = ws.ml[at];
+    }
+  };
+  load(w0 + row);
   float top = -INFINITY;
   for (int32_t w = w0 + threadIdx.x; w <= w1; w += 256) top = fmaxf(top, ws.ml[piece(w)].x);
 #pragma unroll
-  for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+  for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
   if ((threadIdx.x & 63) == 0) top_w[threadIdx.x >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(top_w[0], top_w[1]), fmaxf(top_w[2], top_w[3]));
-  const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float sum = 0.f;
-  for (int32_t w = w0 + row; w <= w1; w += ROWS) {
-    const float2 ml = ws.ml[piece(w)];
-    const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
-    sum += ml.y * f;
-    o += *reinterpret_cast<const f32x4*>(ws.o + piece(w) * D + 4 * lane) * f;
+  for (int32_t w = w0 + row; w <= w1; w += U * ROWS) {
+    if (w > w0 + row) load(w);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (w + u * ROWS > w1) continue;
+      const float f = ml[u].x == top ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - top);
+      sum += ml[u].y * f;
+      o += x[u] * f;
+    }
   }
   part[row][lane] = o;
   if (lane == 0) sums[row] = sum;
@@ -569,7 +592,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeParams p, Decode
 template <int D, bool F8, int NC, bool PAGES16>
 static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   constexpr int kSide = heads_side_by_side(D, F8);
-  const int heads = p.kv_heads % kSide == 0 && p.cache.s_head == D ? kSide : 1;
+  const int64_t most = (int64_t)p.batch * p.kv_heads * ((p.max_rows + 127) / 128);
+  const int heads = p.kv_heads % kSide == 0 && p.cache.s_head == D && most >= 4ll * kCus * waves_per_simd(D, F8, NC) ? kSide : 1;
   const DecodeShape s = decode_shape(p.batch, p.q_heads, p.kv_heads, D, p.max_rows, F8, heads);
   const dim3 grid((uint32_t)((int64_t)s.shares * p.kv_heads * s.blocks / (s.direct ? 1 : heads)));
   if (s.direct) {
