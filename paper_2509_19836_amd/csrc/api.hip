@@ -313,7 +313,7 @@ int check_rope(const burst_rope_t* r, const burst_shape_t* shape, int32_t invers
   if (r->stride_axis > INT64_MAX / 8 || r->stride_b > (INT64_MAX / 4) / shape->batch) return BURST_ERR_INVALID_ARG;
   for (int i = 0; i < r->rotary_dim / 2; ++i) {
     if (r->axis_of_pair[i] >= r->n_axes) return BURST_ERR_INVALID_ARG;
-    out->axes[i / 8] |= (uint16_t)(r->axis_of_pair[i] << (2 * (i % 8)));
+    out->axes[i / 4] |= (uint8_t)(r->axis_of_pair[i] << (2 * (i % 4)));
   }
   out->inv_freq = r->inv_freq;
   out->positions = r->positions;

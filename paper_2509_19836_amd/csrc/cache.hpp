@@ -19,13 +19,25 @@ struct Divider {
   }
 };
 
+// NT: of a tensor that is larger than what stays on the chip until it is next asked for, no line is kept.
+template <class T, bool NT>
+__device__ __forceinline__ T load_as(const void* at) {
+  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const T*>(at));
+  else return *reinterpret_cast<const T*>(at);
+}
+template <bool NT, class T>
+__device__ __forceinline__ void store_as(T x, void* at) {
+  if constexpr (NT) __builtin_nontemporal_store(x, reinterpret_cast<T*>(at));
+  else *reinterpret_cast<T*>(at) = x;
+}
+
 struct RopeDev {
   const float* inv_freq;
   const int32_t* positions;
   int64_t s_axis, s_b;
   int32_t n_axes, rotary_dim;   // rotary_dim 0: no rotation
   int32_t adjacent, inverse;
-  uint16_t axes[8];             // two bits for each of the 8 pairs of a slot
+  uint8_t axes[16];             // two bits for each of four pairs
 };
 
 struct RopeParams {

@@ -124,13 +124,6 @@ __device__ __forceinline__ bf16x8 widened(uint32_t w0, uint32_t w1) {
 }
 
 // A tile's keys and values in a wave's registers.
-// NT: the cache is larger than what stays on the chip from one call to the next: its lines are not kept (read-through, see launch).
-template <class T, bool NT>
-__device__ __forceinline__ T read_once(const char* at) {
-  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const T*>(at));
-  else return *reinterpret_cast<const T*>(at);
-}
-
 template <int D, bool F8, bool NT>
 struct Tile {
   static constexpr int kBytes = F8 ? 1 : 2;
@@ -147,19 +140,19 @@ struct Tile {
   __device__ __forceinline__ static int q_element(int g, int kk) { return F8 ? 64 * (kk / 2) + 16 * g + 8 * (kk & 1) : 32 * kk + 8 * g; }
   __device__ __forceinline__ void load_k(int t, const char* row) {   // of this lane: row 16 t + r, its piece g
 #pragma unroll
-    for (int i = 0; i < KW; ++i) k[t][i] = read_once<u32x4, NT>(row + 64 * i);
+    for (int i = 0; i < KW; ++i) k[t][i] = load_as<u32x4, NT>(row + 64 * i);
   }
   __device__ __forceinline__ void load_v(int e, const char* row) {   // of this lane: key e, elements D / 16 r ..
     if constexpr (VW == 4) {
-      const u32x4 x = read_once<u32x4, NT>(row);
+      const u32x4 x = load_as<u32x4, NT>(row);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[e][i] = x[i];
     } else if constexpr (VW == 2) {
-      const u32x2 x = read_once<u32x2, NT>(row);
+      const u32x2 x = load_as<u32x2, NT>(row);
       v[e][0] = x[0];
       v[e][1] = x[1];
     } else {
-      v[e][0] = read_once<uint32_t, NT>(row);
+      v[e][0] = load_as<uint32_t, NT>(row);
     }
   }
 };
@@ -529,10 +522,10 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
 }
 
 // A (sequence, query head) whose rows several work-groups had: their pieces added up.
-template <int D, int NC>
-__global__ __launch_bounds__(256) void decode_join_kernel(DecodeParams p, DecodeSpace ws, int32_t blocks) {
-  constexpr int LANES = D / 4, ROWS = 256 / LANES;
-  __shared__ float top_w[4];
+template <int D, int NC, int THREADS>
+__global__ __launch_bounds__(THREADS) void decode_join_kernel(DecodeParams p, DecodeSpace ws, int32_t blocks) {
+  constexpr int LANES = D / 4, ROWS = THREADS / LANES;
+  __shared__ float top_w[THREADS / 64];
   __shared__ f32x4 part[ROWS][LANES];
   __shared__ float sums[ROWS];
   const int32_t b = (int32_t)blockIdx.x / p.q_heads, h = (int32_t)blockIdx.x - b * p.q_heads, group = p.q_heads / p.kv_heads;
@@ -549,19 +542,22 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeParams p, Decode
   auto load = [&](int32_t w) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t at = piece(w + u * ROWS < w1 ? w + u * ROWS : w1);
-      x[u] = *reinterpret_cast<const f32x4*>(ws.o + at * D + 4 * lane);
-      ml[u] = ws.ml[at];
+      if (w + u * ROWS <= w1) {
+        const int64_t at = piece(w + u * ROWS);
+        x[u] = *reinterpret_cast<const f32x4*>(ws.o + at * D + 4 * lane);
+        ml[u] = ws.ml[at];
+      }
     }
   };
   load(w0 + row);
   float top = -INFINITY;
-  for (int32_t w = w0 + threadIdx.x; w <= w1; w += 256) top = fmaxf(top, ws.ml[piece(w)].x);
+  for (int32_t w = w0 + threadIdx.x; w <= w1; w += THREADS) top = fmaxf(top, ws.ml[piece(w)].x);
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
   if ((threadIdx.x & 63) == 0) top_w[threadIdx.x >> 6] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(top_w[0], top_w[1]), fmaxf(top_w[2], top_w[3]));
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) top = fmaxf(top, top_w[i]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float sum = 0.f;
   for (int32_t w = w0 + row; w <= w1; w += U * ROWS) {
@@ -605,7 +601,10 @@ static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   else hipLaunchKernelGGL((decode_kernel<D, F8, NC, PAGES16, false, 1>), grid, dim3(64 * kDealtWaves), 0, stream, p, ws, s.blocks, s.shares);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((decode_join_kernel<D, NC>), dim3((uint32_t)(p.batch * p.q_heads)), dim3(256), 0, stream, p, ws, s.blocks);
+  // pieces of a sequence: a share or two where there are as many sequences as shares, all of them where there is one
+  const dim3 joins((uint32_t)(p.batch * p.q_heads));
+  if (s.shares > 4 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 256>), joins, dim3(256), 0, stream, p, ws, s.blocks);
+  else hipLaunchKernelGGL((decode_join_kernel<D, NC, 64>), joins, dim3(64), 0, stream, p, ws, s.blocks);
   return hipGetLastError();
 }
 
