@@ -6,6 +6,7 @@
 #define BURST_ATTN_DIAG_H
 
 #include "burst_attn.h"
+#include "burst_attn_cache.h"
 #include "burst_lm_head.h"
 
 #ifdef __cplusplus
@@ -75,6 +76,11 @@ int burst_attn_launch_plan(int32_t call, int32_t n_steps, const burst_shape_t* s
 /* Host view of the LM head's products over the first sequence tile of a call with this shape (tile_tokens as given; no GPU involved): for
  * the logits, dH and dW the edge of an output tile (128 or 256) and the parts its contraction is split in, out = {edge, parts} x 3. */
 int burst_lm_head_tile_plan(const burst_lm_head_shape_t* shape, int32_t out[6]);
+
+/* How a burst_attn_decode of these sizes is dealt: out[0] shares that the rows of all sequences are dealt to, each a work-group for every key head
+ * or out[1] key heads that lie side by side; out[2] = 1: no dealing, a work-group for every sequence and key head, and out[0] the sequences.
+ * Host only; nothing of the cache is read but its type, head stride and page size. */
+int burst_attn_decode_plan(const burst_shape_t* shape, const burst_cache_t* cache, int32_t out[3]);
 
 #ifdef __cplusplus
 }

@@ -138,6 +138,8 @@ _lib.burst_attn_cache_append.argtypes = [_P(burst_shape_t), _P(burst_cache_t), C
                                          _P(burst_rope_t), C.c_char_p, C.c_char_p, C.c_void_p]
 _lib.burst_attn_decode_workspace_bytes.restype = C.c_int64
 _lib.burst_attn_decode_workspace_bytes.argtypes = [_P(burst_shape_t)]
+_lib.burst_attn_decode_plan.restype = C.c_int
+_lib.burst_attn_decode_plan.argtypes = [_P(burst_shape_t), _P(burst_cache_t), _P(C.c_int32)]
 _lib.burst_attn_decode.restype = C.c_int
 _lib.burst_attn_decode.argtypes = [_P(burst_shape_t), _P(burst_cache_t), C.c_char_p, C.c_void_p, C.c_char_p,
                                    C.c_char_p, C.c_void_p, C.c_int64, C.c_void_p]
@@ -153,7 +155,7 @@ EXPORTS = ["burst_attn_step_fwd", "burst_attn_steps_fwd", "burst_attn_steps_bwd"
            "burst_attn_visible_pairs", "burst_attn_tile_class", "burst_attn_visible_tile_runs", "burst_attn_visible_rows", "burst_attn_mfma_probe", "burst_attn_set_chunk_rows", "burst_attn_chunk_plan", "burst_attn_launch_plan", "burst_attn_status_string", "burst_attn_last_hip_error",
            "burst_attn_version", "burst_lm_head_workspace_bytes", "burst_lm_head_loss",
            "burst_lm_head_static_scratch_bytes", "burst_lm_head_tile_plan", "burst_lm_head_loss_noalloc",
-           "burst_attn_rope", "burst_attn_cache_append", "burst_attn_decode_workspace_bytes", "burst_attn_decode"]
+           "burst_attn_rope", "burst_attn_cache_append", "burst_attn_decode_workspace_bytes", "burst_attn_decode", "burst_attn_decode_plan"]
 
 
 class BurstError(RuntimeError):
@@ -576,6 +578,13 @@ def burst_attn_decode(shp, cache, q, o, lse=None, workspace=None, first_row=None
     ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check(_lib.burst_attn_decode(shp, cache, _packed(q, device, batch, 1, q_heads, d), _numbers(first_row, device, batch),
                                   _packed(o, device, batch, 1, q_heads, d), lse, ws, n, stream))
+
+
+def burst_attn_decode_plan(shp, cache):
+    """(shares, key heads that a work-group takes together, whether nothing is dealt) of a burst_attn_decode (diagnostics)."""
+    out = (C.c_int32 * 3)()
+    _check(_lib.burst_attn_decode_plan(shp, cache, out))
+    return out[0], out[1], bool(out[2])
 
 
 def burst_attn_mfma_probe(random_operands, iterations, stream=None):

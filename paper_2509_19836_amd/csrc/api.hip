@@ -621,8 +621,8 @@ int burst_attn_cache_append(const burst_shape_t* shape, const burst_cache_t* cac
 static int check_decode_shape(const burst_shape_t* shape) {
   BURST_TRY(check_shape(shape));
   if (shape->sq != 1) return BURST_ERR_INVALID_ARG;
-  // 32-bit numbers of (sequence, head) pairs and of units of 128 rows
-  if ((int64_t)shape->batch * shape->q_heads > (1 << 24) || shape->batch * (shape->sk / 128 + 1) > INT32_MAX) return BURST_ERR_UNSUPPORTED;
+  // 32-bit numbers of (sequence, head) pairs and of units of 32 to 128 rows
+  if ((int64_t)shape->batch * shape->q_heads > (1 << 24) || shape->batch * (shape->sk / 32 + 1) > INT32_MAX) return BURST_ERR_UNSUPPORTED;
   return BURST_OK;
 }
 
@@ -658,6 +658,21 @@ int burst_attn_decode(const burst_shape_t* shape, const burst_cache_t* cache, co
   p.workspace = workspace;
   const hipError_t e = launch_decode(p, (hipStream_t)hip_stream);
   return e == hipSuccess ? BURST_OK : hip_fail(e);
+}
+
+int burst_attn_decode_plan(const burst_shape_t* shape, const burst_cache_t* cache, int32_t out[3]) {
+  BURST_TRY(check_decode_shape(shape));
+  DecodeParams p;
+  std::memset(&p, 0, sizeof(p));
+  BURST_TRY(check_cache(cache, shape, &p.cache));
+  if (!out || shape->sk > (int64_t)p.cache.table_cols * p.cache.page_rows) return BURST_ERR_INVALID_ARG;
+  p.batch = shape->batch;
+  p.q_heads = shape->q_heads;
+  p.kv_heads = shape->kv_heads;
+  p.head_dim = shape->head_dim;
+  p.max_rows = (int32_t)shape->sk;
+  decode_plan(p, out);
+  return BURST_OK;
 }
 
 static int fill_common(int32_t dev_i, int32_t shard_j, int32_t G, int64_t N, burst_mask_t* out) {

@@ -95,6 +95,7 @@ struct DecodeParams {
 hipError_t launch_rope(const RopeParams& p, hipStream_t stream);
 hipError_t launch_cache_append(const AppendParams& p, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams& p, hipStream_t stream);
+void decode_plan(const DecodeParams& p, int32_t out[3]);   // burst_attn_decode_plan
 int64_t decode_workspace_bytes(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t max_rows);
 
 }  // namespace burst

@@ -205,48 +205,62 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
   } else {
     __shared__ int32_t scan[kWaves];
     __shared__ FirstUnit found;
-    int32_t total = 0;   // (below 2^31, checked on the host)
-    SeqRows mine = {};
-    for (int32_t b0 = 0; b0 < p.batch; b0 += 256) {
-      mine = b0 + tid < p.batch ? seq_rows_of(p, b0 + tid, kUnit) : SeqRows{};
-      int32_t sum = mine.units;
+    auto upto = [&](int32_t x) {   // sum over this lane and the ones below
 #pragma unroll
-      for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-      if (lane == 0) scan[wave] = sum;
-      __syncthreads();
-      for (int w = 0; w < kWaves; ++w) total += scan[w];
-      __syncthreads();
-    }
-    deal.init(__builtin_amdgcn_readfirstlane(total), shares);
-    unit = deal.first(share);
-    left = deal.first(share + 1) - unit;
-    if (left == 0) return;
-    int32_t passed = 0;
-    for (int32_t b0 = 0; b0 < p.batch; b0 += 256) {
-      if (p.batch > 256) mine = b0 + tid < p.batch ? seq_rows_of(p, b0 + tid, kUnit) : SeqRows{};
-      int32_t upto = mine.units;
-#pragma unroll
-      for (int x = 1; x < 64; x <<= 1) {
-        const int32_t y = __shfl_up(upto, x, 64);
-        upto += lane >= x ? y : 0;
+      for (int s = 1; s < 64; s <<= 1) {
+        const int32_t y = __shfl_up(x, s, 64);
+        x += lane >= s ? y : 0;
       }
-      if (lane == 63) scan[wave] = upto;
-      __syncthreads();
-      int32_t begin = passed + upto - mine.units;
-      for (int w = 0; w < kWaves; ++w) {
-        begin += w < wave ? scan[w] : 0;
-        passed += scan[w];
+      return x;
+    };
+    if (p.batch <= 64) {   // each wave by itself
+      const SeqRows mine = lane < p.batch ? seq_rows_of(p, lane, kUnit) : SeqRows{};
+      const int32_t end = upto(mine.units), begin = end - mine.units;
+      deal.init(__builtin_amdgcn_readlane(end, 63), shares);
+      unit = deal.first(share);
+      left = deal.first(share + 1) - unit;
+      if (left == 0) return;
+      b = __builtin_ctzll(__ballot(begin <= unit && unit < end));   // (one lane)
+      at = unit - __builtin_amdgcn_readlane(begin, b);
+      seq = SeqRows{__builtin_amdgcn_readlane(mine.lo, b), __builtin_amdgcn_readlane(mine.hi, b), __builtin_amdgcn_readlane(mine.start, b),
+                    __builtin_amdgcn_readlane(mine.units, b)};
+    } else {
+      int32_t total = 0;   // (below 2^31, checked on the host)
+      SeqRows mine = {};
+      for (int32_t b0 = 0; b0 < p.batch; b0 += 256) {
+        mine = b0 + tid < p.batch ? seq_rows_of(p, b0 + tid, kUnit) : SeqRows{};
+        const int32_t sum = upto(mine.units);
+        if (lane == 63) scan[wave] = sum;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) total += scan[w];
+        __syncthreads();
       }
-      if (begin <= unit && unit < begin + mine.units) found = FirstUnit{mine, b0 + tid, unit - begin};   // (one thread)
-      __syncthreads();
-      if (passed > unit) break;
+      deal.init(__builtin_amdgcn_readfirstlane(total), shares);
+      unit = deal.first(share);
+      left = deal.first(share + 1) - unit;
+      if (left == 0) return;
+      int32_t passed = 0;
+      for (int32_t b0 = 0; b0 < p.batch; b0 += 256) {
+        if (p.batch > 256) mine = b0 + tid < p.batch ? seq_rows_of(p, b0 + tid, kUnit) : SeqRows{};
+        const int32_t sum = upto(mine.units);
+        if (lane == 63) scan[wave] = sum;
+        __syncthreads();
+        int32_t begin = passed + sum - mine.units;
+        for (int w = 0; w < kWaves; ++w) {
+          begin += w < wave ? scan[w] : 0;
+          passed += scan[w];
+        }
+        if (begin <= unit && unit < begin + mine.units) found = FirstUnit{mine, b0 + tid, unit - begin};   // (one thread)
+        __syncthreads();
+        if (passed > unit) break;
+      }
+      b = __builtin_amdgcn_readfirstlane(found.b);
+      seq.lo = __builtin_amdgcn_readfirstlane(found.seq.lo);
+      seq.hi = __builtin_amdgcn_readfirstlane(found.seq.hi);
+      seq.start = __builtin_amdgcn_readfirstlane(found.seq.start);
+      seq.units = __builtin_amdgcn_readfirstlane(found.seq.units);
+      at = __builtin_amdgcn_readfirstlane(found.at);
     }
-    b = __builtin_amdgcn_readfirstlane(found.b);
-    seq.lo = __builtin_amdgcn_readfirstlane(found.seq.lo);
-    seq.hi = __builtin_amdgcn_readfirstlane(found.seq.hi);
-    seq.start = __builtin_amdgcn_readfirstlane(found.seq.start);
-    seq.units = __builtin_amdgcn_readfirstlane(found.seq.units);
-    at = __builtin_amdgcn_readfirstlane(found.at);
   }
 
   const uint32_t row_bytes = (uint32_t)p.cache.s_row * kBytes;
@@ -536,7 +550,7 @@ __global__ __launch_bounds__(THREADS) void decode_join_kernel(DecodeParams p, De
   const int32_t per_seq = p.kv_heads * blocks, hb = hk * blocks + cb;
   auto piece = [&](int32_t w) { return (2 * ((int64_t)w * per_seq + hb) + (w == w0 ? skip : 0)) * ws.columns + c; };
   const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
-  constexpr int U = 8;   // pieces under way for a thread; the first ones while the largest maximum is looked for
+  constexpr int U = THREADS > 256 ? 4 : 8;   // pieces under way for a thread; the first ones while the largest maximum is looked for
   f32x4 x[U];
   float2 ml[U];
   auto load = [&](int32_t w) {
@@ -574,6 +588,7 @@ __global__ __launch_bounds__(THREADS) void decode_join_kernel(DecodeParams p, De
   if (lane == 0) sums[row] = sum;
   __syncthreads();
   if (row != 0) return;
+#pragma unroll 4
   for (int i = 1; i < ROWS; ++i) {
     o += part[i][lane];
     sum += sums[i];
@@ -585,11 +600,29 @@ __global__ __launch_bounds__(THREADS) void decode_join_kernel(DecodeParams p, De
   if (lane == 0 && p.lse.ptr) p.lse.ptr[b * p.lse.sb + h * p.lse.sh] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
 }
 
+// Heads whose rows a work-group takes together: several where they lie side by side and there are four units of 128 rows and more for each
+// work-group, by the bound.  32 sequences of 16384 rows, 8 heads in e4m3: 223 us one by one, 204 in fours; 16 in bf16: 206 and 188 in
+// twos; 16 heads of 64: 209 and 186 in fours.  A work-group has a piece for each of them, so short ones lose: one sequence, 8 heads of 128 in
+// bf16, 8192 rows 19.7 and 22.2, 32768 rows 38.5 and 38.6, 65536 rows 62 and 60.
+static int heads_together(const DecodeParams& p) {
+  const int side = heads_side_by_side(p.head_dim, p.cache.is_f8 != 0);
+  const int64_t most = (int64_t)p.batch * p.kv_heads * ((p.max_rows + 127) / 128);
+  const int waves = waves_per_simd(p.head_dim, p.cache.is_f8 != 0, columns_of(p.q_heads / p.kv_heads) / 16);
+  return p.kv_heads % side == 0 && p.cache.s_head == p.head_dim && most >= 4ll * kCus * waves ? side : 1;
+}
+
+void decode_plan(const DecodeParams& p, int32_t out[3]) {
+  const int heads = heads_together(p);
+  const DecodeShape s = decode_shape(p.batch, p.q_heads, p.kv_heads, p.head_dim, p.max_rows, p.cache.is_f8 != 0, heads);
+  out[0] = s.shares;
+  out[1] = s.direct ? 1 : heads;
+  out[2] = s.direct;
+}
+
 template <int D, bool F8, int NC, bool PAGES16>
 static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   constexpr int kSide = heads_side_by_side(D, F8);
-  const int64_t most = (int64_t)p.batch * p.kv_heads * ((p.max_rows + 127) / 128);
-  const int heads = p.kv_heads % kSide == 0 && p.cache.s_head == D && most >= 4ll * kCus * waves_per_simd(D, F8, NC) ? kSide : 1;
+  const int heads = heads_together(p);
   const DecodeShape s = decode_shape(p.batch, p.q_heads, p.kv_heads, D, p.max_rows, F8, heads);
   const dim3 grid((uint32_t)((int64_t)s.shares * p.kv_heads * s.blocks / (s.direct ? 1 : heads)));
   if (s.direct) {
@@ -603,7 +636,8 @@ static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   if (e != hipSuccess) return e;
   // pieces of a sequence: a share or two where there are as many sequences as shares, all of them where there is one
   const dim3 joins((uint32_t)(p.batch * p.q_heads));
-  if (s.shares > 4 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 256>), joins, dim3(256), 0, stream, p, ws, s.blocks);
+  if (s.shares > 64 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 1024>), joins, dim3(1024), 0, stream, p, ws, s.blocks);
+  else if (s.shares > 4 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 256>), joins, dim3(256), 0, stream, p, ws, s.blocks);
   else hipLaunchKernelGGL((decode_join_kernel<D, NC, 64>), joins, dim3(64), 0, stream, p, ws, s.blocks);
   return hipGetLastError();
 }
