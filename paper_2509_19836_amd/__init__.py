@@ -6,7 +6,7 @@ touches neither the GPU nor the shared library.
 """
 import importlib
 
-__all__ = ["binding", "workloads", "build"]
+__all__ = ["binding", "workloads", "build", "ring", "decode"]
 
 
 def __getattr__(name):
