@@ -439,10 +439,9 @@ def burst_lm_head_tile_plan(shp):
 
 def _current(stream):
     """The stream to use (the current one, or a given one of the current device) and the number of its device."""
-    if stream is None:
-        s = torch.cuda.current_stream()
-        return s.cuda_stream, s.device_index
-    return stream, torch.cuda.current_device()
+    device = torch.cuda.current_device()
+    # (the handle alone: torch.cuda.current_stream() makes an object of it, 2.8 us of the 9 that a call took)
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream, device
 
 
 def _check_device(device, *tensors):

@@ -326,7 +326,7 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
     auto place = [&](int32_t row0, const int32_t (&page)[2], TilePlace& x) {
       // rows of the tile that the sequence has
       const int32_t below = seq.hi - row0, above = seq.lo - row0;
-      uint32_t seen = below >= 32 ? ~0u : (1u << below) - 1u;
+      uint32_t seen = below >= 32 ? ~0u : below > 0 ? (1u << below) - 1u : 0u;
       if (above > 0) seen &= ~0u << above;   // (start is at most 31 before lo)
       if constexpr (PAGES16) {
 #pragma unroll
