@@ -64,7 +64,7 @@ int burst_attn_rope(const burst_shape_t* shape, const burst_rope_t* rope, const 
  * more) is no error: its rows are not written by an append, and not seen by the attention.
  * e4m3 holds numbers over a scale of their head: the value is number * k_scale[kv_head] (v_scale); NULL: 1.  The scales are the
  * caller's, positive; numbers beyond +-448 are stored as +-448 (infinities too), NaN stays NaN.  With bf16 the scales must be NULL.
- * Pages of a multiple of 16 rows are read fastest.
+ * Pages of a multiple of 16 rows are read fastest, and heads whose rows lie one after the other in a page (head stride above row stride).
  */
 typedef struct {
   burst_tensor_t k, v;
@@ -98,8 +98,10 @@ int burst_attn_cache_append(const burst_shape_t* shape, const burst_cache_t* cac
  *     S_t = scale * q . K_t;  Lse = log sum exp S_t (natural log);  O = sum exp(S_t - Lse) V_t;   without a row O = 0, Lse = -inf.
  * q is bf16 [batch, 1, q_heads, head_dim], o bf16 or fp32 of that shape, lse [batch, q_heads, 1], or NULL: not wanted.
  * shape: sq must be 1; sk is a bound on every sequence's rows, at most table_cols * page_rows (INVALID_ARG): rows at and behind it are
- * not seen.  Work is dealt by the rows that are there, not by the bound.  O is exact to fp32 rounding before it is cast: the numbers
- * exp(S - Lse) are multiplied in two bf16 parts.  A row's result depends on the other sequences of the batch by the order of fp32 sums alone.
+ * not seen.  batch * q_heads above 2^21, or batch * sk of about 2^36 and more: UNSUPPORTED.  Work is dealt by the rows that are there, not by
+ * the bound; but a bound that keeps all keys and values of a head within 256 KiB (512 with 256 (sequence, key head) pairs and more) makes the call
+ * one launch instead of two.  O is exact to fp32 rounding before it is cast: the numbers
+ * exp(S - Lse) are multiplied in two bf16 parts.  A row's result depends on the other sequences of the batch by roundings in fp32 alone.
  * Rows that are not seen may hold anything, NaN too.
  * workspace: burst_attn_decode_workspace_bytes(shape) bytes, 256-byte aligned, contents on entry irrelevant, on return unspecified; calls
  * that share one must be ordered on one stream.  The size depends on batch, the heads, head_dim and sk; it is 0 for some shapes, for which

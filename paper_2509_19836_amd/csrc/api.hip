@@ -621,8 +621,8 @@ int burst_attn_cache_append(const burst_shape_t* shape, const burst_cache_t* cac
 static int check_decode_shape(const burst_shape_t* shape) {
   BURST_TRY(check_shape(shape));
   if (shape->sq != 1) return BURST_ERR_INVALID_ARG;
-  // 32-bit numbers of (sequence, head) pairs and of units of 32 to 128 rows
-  if ((int64_t)shape->batch * shape->q_heads > (1 << 24) || shape->batch * (shape->sk / 32 + 1) > INT32_MAX) return BURST_ERR_UNSUPPORTED;
+  // a launch of less than 2^32 threads, 512 of them for each (sequence, head); 32-bit numbers of units of 32 to 128 rows
+  if ((int64_t)shape->batch * shape->q_heads > (1 << 21) || shape->batch * (shape->sk / 32 + 1) > INT32_MAX) return BURST_ERR_UNSUPPORTED;
   return BURST_OK;
 }
 

@@ -8,14 +8,21 @@
 //   take 64 bytes each of 16 rows (an A operand as it is), 16 lanes of a V load a whole row.  Lane (r, g) then has for 8 keys the same
 //   D / 16 elements of V, and one v_perm for every two of them makes them the A operand whose k index is the key: the keys that S^T leaves
 //   in this lane's accumulators (16 (e / 4) + 4g + e % 4), so P needs no exchange between lanes either.
-//   The running maximum of a column is a whole number (base 2), so that a rescale by 2^n changes no bit of P and O, and which
-//   rows another wave or work-group took has no influence but the order of fp32 sums.  P goes in whole, as the three bf16 numbers that its
-//   24 bits are; the matrix pipe has the time for it.
+//   The running maximum of a column is a whole number (base 2), so that a rescale by 2^n changes no bit of P and O, and which rows
+//   another wave or work-group took has no influence but roundings in fp32 (of S minus the maximum, and the order of sums).  P goes in whole, as the three bf16 numbers that its
+//   24 bits are (in two parts O was 4.9e-6 off 64 bits, in three 1.1e-6, as elementary operations in 32 bits; the time is the same: the matrix
+//   pipe is busy a sixth of it).
 //
-//   Work is cut into units of 128 rows (a tile for each wave), numbered over (sequence, key head, rows), and dealt evenly to as many
-//   work-groups as the chip holds at once, whatever the sequences' lengths are: each finds its first unit by a scan over
-//   the sequences.  A piece that is a whole (sequence, key head) is written out; what a work-group has of others goes to the workspace,
-//   two pieces at most, and decode_join_kernel adds the pieces up in a fixed order.
+//   Work is cut into units of a tile for each wave and numbered over (sequence, rows).  The units are dealt evenly to shares, a work-group each for
+//   every key head, as many as the chip holds at once, whatever the sequences' lengths are: each finds its first unit by a scan
+//   over the sequences.  A piece that is a whole (sequence, key head) is written out; what a work-group has of others goes to the
+//   workspace, two pieces at most, and decode_join_kernel adds the pieces up in a fixed order.  Half as many work-groups as fit: e4m3 212 -> 239
+//   us, one and a half times as many 212 -> 232, twice as many 228.  Two tiles under way in a wave instead of one: no gain (the
+//   CU's own rate of loads, about 50 GB/s, is what a short sequence waits for, and the memory a long one).
+//
+// Measured (rows x key heads, a cache of its own for each of three calls in turn): 131072 x 32 bf16 319 us, 6.73 TB/s (a copy reaches 5.2, a
+// fill 6.9); 32 sequences of 32768 and fewer x 8 in e4m3 135 us, 5.3 TB/s (128-byte rows of heads side by side; head by head 5.7); 64
+// of 4096 and fewer x 8 64 us, 5.1 TB/s; 32768 x 8 32 us, 4.2 TB/s, of which 5 us are the second kernel and 6 the first loads.
 #include "cache.hpp"
 #include "kernels.hpp"
 #include "mfma16.hpp"
@@ -31,7 +38,7 @@ constexpr int kTileRows = 32, kDealtWaves = 4;
 constexpr int kDirectWaves = 8;
 constexpr float kStale = 8.f;   // a maximum may fall behind by a factor of 2^8: P, O and their sums stay far inside fp32
 constexpr int kCus = 256;
-// Waves that share a SIMD, by the registers that one takes: work-groups of four waves that share a CU.
+// Waves that share a SIMD, by the registers that one takes (also: work-groups of four waves that share a CU).
 constexpr int waves_per_simd(int head_dim, bool f8, int nc) { return nc == 2 ? 2 : 2 + (head_dim == 64) + f8; }
 
 // What a sequence's share of the work is.  It starts at a multiple of the tile, so that the halves of a tile lie in one page each where
@@ -93,7 +100,10 @@ static DecodeShape decode_shape(int32_t batch, int32_t q_heads, int32_t kv_heads
   s.blocks = (group + wide - 1) / wide;
   s.columns = group < wide ? group : wide;
   const int64_t per_seq = (int64_t)kv_heads * s.blocks, unit = kTileRows * kDealtWaves / heads, max_units = (max_rows + unit - 1) / unit;
-  // The line between the two: a work-group for each (sequence, key head) saves the scan and the second kernel and reads its rows by itself.
+  // The line between the two: a work-group for each (sequence, key head) saves the scan and the second kernel, and reads its rows by itself.  bf16,
+  // heads of 128, direct and dealt: one sequence x 8 heads, 512 rows 9.7 and 11.4 us, 1024 rows 14.3 and 11.5; heads of 64, 1024 rows 10.2
+  // and 10.4; e4m3, 32 sequences x 8, 1024 rows 16.2 and 24, 2048 rows 34.5 and 41; bf16, 64 sequences x 8, 1024 rows 56 and 55, of
+  // that and less 39 and 38.
   const int64_t head_bytes = max_rows * head_dim * (f8 ? 2 : 4);
   s.direct = head_bytes <= (batch * per_seq < kCus ? 256 << 10 : 512 << 10);
   const int64_t fit = std::max<int64_t>(1, kCus * waves_per_simd(head_dim, f8, wide / 16) * heads / per_seq);
@@ -123,7 +133,9 @@ __device__ __forceinline__ bf16x8 widened(uint32_t w0, uint32_t w1) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A tile's keys and values in a wave's registers.
+// A tile's keys and values in a wave's registers.  NT (where work is dealt): the lines are not kept, as there are more than the chip keeps until the
+// next call; 131072 rows x 32 heads 374 -> 334 us, 16 x 16384 x 8 202 -> 179, 32768 x 8 38.9 -> 35.9 (head by head).  Where a sequence
+// is short they are, for the next call: 1024 rows x 8 heads 14.6 us kept, 19.8 not.
 template <int D, bool F8, bool NT>
 struct Tile {
   static constexpr int kBytes = F8 ? 1 : 2;
@@ -634,7 +646,8 @@ static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   else hipLaunchKernelGGL((decode_kernel<D, F8, NC, PAGES16, false, 1>), grid, dim3(64 * kDealtWaves), 0, stream, p, ws, s.blocks, s.shares);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // pieces of a sequence: a share or two where there are as many sequences as shares, all of them where there is one
+  // Threads for the pieces of a sequence, a share or two where there are as many sequences as shares, all of them where there is one.  64 sequences,
+  // 64 shares: 69 us with 256 threads, 65.5 with 64; one sequence of one head, 512 shares: the join alone 12 us with 256, 8 with 1024.
   const dim3 joins((uint32_t)(p.batch * p.q_heads));
   if (s.shares > 64 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 1024>), joins, dim3(1024), 0, stream, p, ws, s.blocks);
   else if (s.shares > 4 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 256>), joins, dim3(256), 0, stream, p, ws, s.blocks);

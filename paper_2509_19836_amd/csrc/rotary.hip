@@ -204,12 +204,6 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams p, TokenShare shar
   if (p.k.ptr) turn_tensor<NT>(p.rope, t, at, p.k, p.k_out, b, row, head, step, p.kv_heads);
 }
 
-static TokenShare token_share(int32_t head_dim, int32_t heads) {
-  TokenShare s{head_dim == 128 ? 3 : 2, 0};
-  while (s.slots_log2 + s.heads_log2 < 8 && (4 << s.heads_log2) < heads) ++s.heads_log2;
-  return s;
-}
-
 // Whether lines are kept: not where a call moves more than the 256 MiB that the chip keeps and every access takes whole lines, 8 threads of 16
 // bytes.  16384 rows x 64 heads of 128, bf16: 102 us kept, 94 not; 4096 x 40: 17.1 kept, 18.6 not; with half lines, of 64 elements
 // turned out of 128, 103 kept and 113 not.  (The 32 bytes that a thread takes of fp32 are two accesses: 172 and 157 us from fp32 to bf16, 16384
@@ -218,16 +212,29 @@ static bool streams(int64_t bytes, int32_t head_dim, const RopeDev& r) {
   return bytes > ((int64_t)256 << 20) && head_dim == 128 && (r.rotary_dim == 128 || r.rotary_dim == 0);
 }
 
+// Heads that a thread takes one after the other: the more, the fewer times sine and cosine are formed; the fewer, the more threads there are.  One
+// where these do not fill the chip twice over (256 tokens of 40 heads: 6.0 us, by fours 6.8; 16 tokens 5.6, 6.5), two of bf16 where
+// lines are not kept and there are about as many key heads, or threads would wait while others take those (16384 x 32 + 32 heads: 90.6 us, by
+// fours 95.4, by ones 121; appended, 16000 x 32 + 32: 137, by fours 144, but 16384 x 64 + 8: 132 and 115), four otherwise (4096 x 40: 16.7 us, by twos 18.2, by
+// eights 17.9; 4 x 8192 x 24 heads of 64: 43.1, 43.3, 46.8; fp32 to bf16, 16384 x 72: 159, 161, 162).
+static TokenShare token_share(int32_t head_dim, int32_t heads, int64_t tokens, bool by_twos) {
+  TokenShare s{head_dim == 128 ? 3 : 2, 0};
+  const int64_t all = tokens * heads * (head_dim / 16);
+  const int each = all <= 2 * 256 * 256 ? 1 : by_twos ? 2 : 4;
+  while (s.slots_log2 + s.heads_log2 < 8 && (each << s.heads_log2) < heads) ++s.heads_log2;
+  return s;
+}
+
 hipError_t launch_rope(const RopeParams& p, hipStream_t stream) {
   const int64_t total = (int64_t)p.batch * p.sq;
   if (total == 0) return hipSuccess;
-  const TokenShare share = token_share(p.head_dim, p.q_heads);
-  const int64_t grid = (total + share.tokens() - 1) / share.tokens();
   auto bytes = [&](const TensorDev& x, const TensorDev& y, int32_t heads) {
     return x.ptr ? total * heads * p.head_dim * ((x.is_f32 ? 4 : 2) + (y.is_f32 ? 4 : 2)) : (int64_t)0;
   };
   const bool f32_to_f32 = (p.q.is_f32 && p.q_out.is_f32) || (p.k.ptr && p.k.is_f32 && p.k_out.is_f32);
   const bool nt = !f32_to_f32 && streams(bytes(p.q, p.q_out, p.q_heads) + bytes(p.k, p.k_out, p.kv_heads), p.head_dim, p.rope);
+  const TokenShare share = token_share(p.head_dim, p.q_heads, total, nt && !p.q.is_f32 && 2 * p.kv_heads >= p.q_heads);
+  const int64_t grid = (total + share.tokens() - 1) / share.tokens();
   if (nt) hipLaunchKernelGGL(rope_kernel<true>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
   else hipLaunchKernelGGL(rope_kernel<false>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
   return hipGetLastError();
@@ -268,10 +275,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendParams p, Token
 hipError_t launch_cache_append(const AppendParams& p, hipStream_t stream) {
   const int64_t total = (int64_t)p.batch * p.sq;
   if (total == 0) return hipSuccess;
-  const TokenShare share = token_share(p.head_dim, p.q.ptr ? p.q_heads : p.kv_heads);
-  const int64_t grid = (total + share.tokens() - 1) / share.tokens();
   const int64_t bytes = total * p.head_dim * ((p.q.ptr ? 4 * p.q_heads : 0) + 2 * p.kv_heads * (p.cache.is_f8 ? 3 : 4));
-  if (streams(bytes, p.head_dim, p.rope)) hipLaunchKernelGGL(cache_append_kernel<true>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
+  const bool nt = streams(bytes, p.head_dim, p.rope);
+  const TokenShare share = token_share(p.head_dim, p.q.ptr ? p.q_heads : p.kv_heads, total, nt && (!p.q.ptr || 2 * p.kv_heads >= p.q_heads));
+  const int64_t grid = (total + share.tokens() - 1) / share.tokens();
+  if (nt) hipLaunchKernelGGL(cache_append_kernel<true>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
   else hipLaunchKernelGGL(cache_append_kernel<false>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
   return hipGetLastError();
 }

@@ -266,7 +266,7 @@ def test_offsets_beyond_32_bits(lib):
 
 
 def test_a_row_does_not_depend_on_its_batch(lib):
-    """The same sequence alone and among others: fp32 sums in another order, 2^-20 of O at most (P's bits are the same)."""
+    """The same sequence alone and among others: other roundings in fp32 (S minus another maximum, sums in another order), 2^-20 of O at most."""
     rng = np.random.Generator(np.random.PCG64(wl.BASE_SEED + 83200))
     rows = [1777, 5, 900, 3100, 64, 1777]
     P = Paged(lib, rng, rows, 16, 2, 128)
