@@ -646,11 +646,12 @@ static hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   else hipLaunchKernelGGL((decode_kernel<D, F8, NC, PAGES16, false, 1>), grid, dim3(64 * kDealtWaves), 0, stream, p, ws, s.blocks, s.shares);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // Threads for the pieces of a sequence, a share or two where there are as many sequences as shares, all of them where there is one.  64 sequences,
-  // 64 shares: 69 us with 256 threads, 65.5 with 64; one sequence of one head, 512 shares: the join alone 12 us with 256, 8 with 1024.
+  // Threads for the pieces of a sequence: a share or two where there are as many sequences as shares, all of them where there is one.  A wave takes
+  // 16 pieces (heads of 128) at once.  64 sequences, 64 shares: 69 us with 256 threads, 65.5 with 64; one sequence of one head, 512 shares:
+  // the join alone 12 us with 256, 8 with 1024.
   const dim3 joins((uint32_t)(p.batch * p.q_heads));
   if (s.shares > 64 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 1024>), joins, dim3(1024), 0, stream, p, ws, s.blocks);
-  else if (s.shares > 4 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 256>), joins, dim3(256), 0, stream, p, ws, s.blocks);
+  else if (s.shares > 16 * p.batch) hipLaunchKernelGGL((decode_join_kernel<D, NC, 256>), joins, dim3(256), 0, stream, p, ws, s.blocks);
   else hipLaunchKernelGGL((decode_join_kernel<D, NC, 64>), joins, dim3(64), 0, stream, p, ws, s.blocks);
   return hipGetLastError();
 }
