@@ -28,7 +28,7 @@ class PagedCache:
 
     def grow(self, new_rows):
         """Room for new_rows[b] more rows of each sequence, which count from now on: the next append fills them (in every layer that shares
-        the table).  Raises, and changes nothing, where pages run out or a sequence would pass max_rows."""
+        the table), on the current stream.  Raises, and changes nothing, where pages run out or a sequence would pass max_rows."""
         lengths = [n + m for n, m in zip(self.lengths, new_rows, strict=True)]
         if min(new_rows) < 0 or max(lengths) > self.max_rows:
             raise ValueError(f"a sequence has 0 to {self.max_rows} rows")
@@ -45,7 +45,7 @@ class PagedCache:
         self.rows.copy_(torch.tensor(lengths, dtype=torch.int32))
 
     def release(self, b):
-        """Sequence b is over: its pages are free again."""
+        """Sequence b is over: its pages are free again, on the current stream."""
         self.free += reversed(self.pages[b])
         self.pages[b], self.lengths[b] = [], 0
         self.table[b] = -1
@@ -53,11 +53,11 @@ class PagedCache:
 
 
 def append(cache, q, k, v, rope, q_out, new_rows=None, stream=None):
-    """The rows that the cache has grown by: k (turned) and v into it, q (turned) into q_out; new_rows as in grow (None: all of k)."""
+    """The rows that the cache has grown by: k (turned) and v into it, q (turned) into q_out; new_rows: those numbers as an int32 tensor on the
+    device, that lives until the call has run (None: all rows of k)."""
     B, n, Hq, d = q.shape
-    new = None if new_rows is None else torch.tensor(new_rows, dtype=torch.int32).to(q.device)
-    lib.burst_attn_cache_append(lib.shape(B, Hq, k.shape[2], d, n, 0, 1.0), cache.handle, k, v, new_rows=new, rope=rope, q=q, q_out=q_out,
-                                stream=stream)
+    lib.burst_attn_cache_append(lib.shape(B, Hq, k.shape[2], d, n, 0, 1.0), cache.handle, k, v, new_rows=new_rows, rope=rope, q=q,
+                                q_out=q_out, stream=stream)
 
 
 def workspace(cache, q_heads):

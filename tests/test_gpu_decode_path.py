@@ -93,6 +93,6 @@ def test_pages_are_handed_out_and_come_back(lib):
     assert sorted(sum(cache.pages, []) + cache.free) == list(range(6))
     x = torch.ones(3, 16, 1, 64, device="cuda", dtype=torch.bfloat16)
     decode.append(cache, x, x, x, lib.rope(torch.zeros(1, 3, 16, device="cuda", dtype=torch.int32), torch.ones(32, device="cuda")), torch.empty_like(x),
-                  new_rows=[0, 0, 16])
+                  new_rows=torch.tensor([0, 0, 16], dtype=torch.int32, device="cuda"))
     k = cache.handle._tensors[0]
     assert (k[cache.pages[2][1]] == 1).all()

@@ -465,3 +465,28 @@ def test_shards_of_a_ring_joined(lib):
     O, L = oc.mha_attention_fwd(q_host[:, None], hp.widen(k), hp.widen(v), 0.09)
     assert np.abs(o.double().cpu().numpy() - O).max() <= 2e-5 * np.abs(O).max() + 1e-6
     assert np.abs(lse.double().cpu().numpy() - L).max() <= 1e-5
+
+
+def test_keys_alone_are_turned_and_one_query_head_for_each(lib):
+    """An append without queries; and the bits of one with them."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    k, v, q = (torch.randn(2, 7, 3, 64, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(3))
+    rope = lib.rope(torch.randint(0, 9999, (1, 2, 7), generator=gen, device="cuda", dtype=torch.int32), torch.from_numpy(tr._frequencies(32)).cuda())
+    pages = []
+    for with_q in (False, True):
+        P = Paged(lib, np.random.Generator(np.random.PCG64(5)), [20, 7], 16, 3, 64)
+        args = dict(q=q, q_out=torch.empty_like(q)) if with_q else {}
+        lib.burst_attn_cache_append(lib.shape(2, 3, 3, 64, 7, 0, 1.0), P.cache, k, v, None, rope, **args)
+        pages.append(P)
+    assert all(torch.equal(pages[0].dev[x], pages[1].dev[x]) for x in "kv")
+
+
+@pytest.mark.parametrize("Hq,Hkv,page_rows", [(130, 1, 1 << 12), (97, 97, 16), (512, 4, 80)])
+def test_heads_and_pages_of_unusual_sizes(lib, Hq, Hkv, page_rows):
+    rng = np.random.Generator(np.random.PCG64(wl.BASE_SEED + 83300 + Hq))
+    rows = [700, 0, 3]
+    P = Paged(lib, rng, rows, page_rows, Hkv, 64, spare=1)
+    q, q_host = queries(rng, 3, Hq, 64)
+    o, lse = run_decode(lib, P, q, 0.125, 700, [3, 0, 1])
+    check_decode(o, lse, P.decode(q_host, 0.125, [3, 0, 1]), 700, 64)

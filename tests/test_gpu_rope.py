@@ -160,3 +160,42 @@ def test_far_strides_and_unaligned_plans(lib):
     ref = co.rope(host, pos.reshape(1, 2, 1), freq, [0] * 32)
     angle = co.angles(pos.reshape(1, 2, 1), freq, [0] * 32)
     assert (np.abs(x.double().cpu().numpy() - ref) <= tolerance(host, ref, angle, d, False, True)).all()
+
+
+@pytest.mark.parametrize("q_types,k_types", [(("f32", "bf16"), ("bf16", "f32")), (("bf16", "bf16"), ("f32", "f32"))])
+def test_queries_and_keys_of_types_of_their_own(lib, q_types, k_types):
+    """One launch for both, each tensor with its types: the bits of a launch for each."""
+    import torch
+    types = {"bf16": torch.bfloat16, "f32": torch.float32}
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    n, Hq, Hkv, d = 33, 6, 2, 128
+    x = {"q": torch.randn(1, n, Hq, d, generator=gen, device="cuda").to(types[q_types[0]]),
+         "k": torch.randn(1, n, Hkv, d, generator=gen, device="cuda").to(types[k_types[0]])}
+    empty = lambda name, to: torch.empty_like(x[name], dtype=types[to])
+    together, alone = {"q": empty("q", q_types[1]), "k": empty("k", k_types[1])}, {"q": empty("q", q_types[1]), "k": empty("k", k_types[1])}
+    r = lib.rope(torch.arange(n, device="cuda", dtype=torch.int32).view(1, 1, n), torch.from_numpy(_frequencies(48)).cuda(), adjacent=True)
+    lib.burst_attn_rope(lib.shape(1, Hq, Hkv, d, n, 0, 1.0), r, x["q"], together["q"], x["k"], together["k"])
+    lib.burst_attn_rope(lib.shape(1, Hq, Hq, d, n, 0, 1.0), r, x["q"], alone["q"])
+    lib.burst_attn_rope(lib.shape(1, Hkv, Hkv, d, n, 0, 1.0), r, x["k"], alone["k"])
+    assert torch.equal(together["q"], alone["q"]) and torch.equal(together["k"], alone["k"])
+
+
+def test_captured_and_replayed(lib):
+    """From one graph, with positions that the program changes between replays, and eager calls between: the eager bits every time."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(2, 5, 4, 64, generator=gen, device="cuda").to(torch.bfloat16)
+    pos = torch.zeros(1, 2, 5, device="cuda", dtype=torch.int32)
+    r, shp, y = lib.rope(pos, torch.from_numpy(_frequencies(32)).cuda()), lib.shape(2, 4, 4, 64, 5, 0, 1.0), torch.empty_like(x)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        lib.burst_attn_rope(shp, r, x, y)
+    for turn in range(4):
+        pos += 1000 * turn + 1
+        y.fill_(7.0)
+        graph.replay()
+        got = y.clone()
+        lib.burst_attn_rope(shp, r, x, y)
+        torch.cuda.synchronize()
+        assert torch.equal(got, y) and not torch.equal(got, x)
