@@ -454,14 +454,15 @@ def _check_device(device, *tensors):
 _pack_tensor, _pack_rowvec = struct.Struct("=Qiiqqq").pack, struct.Struct("=Qqq").pack
 
 
-def _packed(t, device, *sizes):
+def _packed(t, device, sizes):
     """The bytes of the burst_tensor_t of a tensor of these sizes on this device, or None."""
     if t is None:
         return None
-    _check_device(device, t)
     stride = t.stride()
     if t.shape != sizes or stride[3] != 1:
         raise ValueError(f"tensor of {sizes} with a contiguous last dimension expected, not {tuple(t.shape)}, strides {stride}")
+    if t.get_device() != device:
+        _check_device(device, t)
     return _pack_tensor(t.data_ptr(), _DTYPES[t.dtype], 0, stride[0], stride[1], stride[2])
 
 
@@ -485,23 +486,23 @@ def rope(positions, inv_freq, rotary_dim=None, adjacent=False, axis_of_pair=None
         raise ValueError("at most 64 pairs")
     r = burst_rope_t(positions.size(0), 2 * pairs, int(adjacent), 0, inv_freq.data_ptr(), _int32(positions, 3),
                      positions.stride(0), positions.stride(1), (C.c_uint8 * 64)(*axes))
-    r._tensors = (positions, inv_freq)
+    r._tensors, r._rows = (positions, inv_freq), tuple(positions.shape[1:])
     return r
 
 
 def _check_positions(r, batch, sq):
-    if r is not None and r._tensors[0].shape[1:] != (batch, sq):
-        raise ValueError(f"positions of {batch} sequences of {sq} rows expected, not {tuple(r._tensors[0].shape[1:])}")
+    if r is not None and r._rows != (batch, sq):
+        raise ValueError(f"positions of {batch} sequences of {sq} rows expected, not {r._rows}")
 
 
 def burst_attn_rope(shp, rope, q, q_out, k=None, k_out=None, inverse=False, stream=None):
     """q, q_out [batch, sq, q_heads, head_dim], k, k_out [batch, sq, kv_heads, head_dim], bf16 or fp32; q_out may be q (in place)."""
     stream, device = _current(stream)
-    batch, sq, q_heads, kv_heads, d = shp.batch, shp.sq, shp.q_heads, shp.kv_heads, shp.head_dim
+    batch, sq, d = shp.batch, shp.sq, shp.head_dim
+    q_sizes, k_sizes = (batch, sq, shp.q_heads, d), (batch, sq, shp.kv_heads, d)
     _check_positions(rope, batch, sq)
-    _check(_lib.burst_attn_rope(shp, rope, _packed(q, device, batch, sq, q_heads, d), _packed(q_out, device, batch, sq, q_heads, d),
-                                _packed(k, device, batch, sq, kv_heads, d), _packed(k_out, device, batch, sq, kv_heads, d),
-                                int(inverse), stream))
+    _check(_lib.burst_attn_rope(shp, rope, _packed(q, device, q_sizes), _packed(q_out, device, q_sizes), _packed(k, device, k_sizes),
+                                _packed(k_out, device, k_sizes), int(inverse), stream))
 
 
 def paged_cache(k, v, table, rows, k_scale=None, v_scale=None):
@@ -517,7 +518,7 @@ def paged_cache(k, v, table, rows, k_scale=None, v_scale=None):
             raise ValueError("scales: kv_heads contiguous fp32 numbers expected")
     c = burst_cache_t(_cache_tensor(k), _cache_tensor(v), k.size(0), k.size(1), table.size(1), _int32(table, 2), table.stride(0),
                       _int32(rows, 1), None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
-    c._tensors = (k, v, table, rows, k_scale, v_scale)
+    c._tensors, c._sizes = (k, v, table, rows, k_scale, v_scale), (rows.size(0), k.size(2), k.size(3))
     return c
 
 
@@ -529,8 +530,7 @@ def _cache_tensor(t):
 
 
 def _check_cache(cache, batch, kv_heads, d):
-    k, _, _, rows, _, _ = cache._tensors
-    if rows.shape[0] != batch or k.shape[2:] != (kv_heads, d):
+    if cache._sizes != (batch, kv_heads, d):
         raise ValueError("the cache has another batch, kv_heads or head_dim than the shape")
 
 
@@ -538,22 +538,24 @@ def _numbers(t, device, batch):
     """The address of an int32 number for each sequence, or None."""
     if t is None:
         return None
-    _check_device(device, t)
-    if t.shape != (batch,):
-        raise ValueError(f"tensor of {(batch,)} expected, not {tuple(t.shape)}")
-    return _int32(t, 1)
+    if t.get_device() != device:
+        _check_device(device, t)
+    if t.dtype != torch.int32 or t.shape != (batch,) or (batch > 1 and t.stride(0) != 1):
+        raise ValueError(f"int32 tensor of {(batch,)} contiguous numbers expected, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    return t.data_ptr()
 
 
 def burst_attn_cache_append(shp, cache, k, v, new_rows=None, rope=None, q=None, q_out=None, stream=None):
     """k, v [batch, sq, kv_heads, head_dim] bf16: sequence b's first new_rows[b] rows (all) become its rows rows[b] - new_rows[b] ..
     rows[b] - 1.  With a rotation the keys are turned, and q [batch, sq, q_heads, head_dim] into q_out."""
     stream, device = _current(stream)
-    batch, sq, q_heads, kv_heads, d = shp.batch, shp.sq, shp.q_heads, shp.kv_heads, shp.head_dim
+    batch, sq, kv_heads, d = shp.batch, shp.sq, shp.kv_heads, shp.head_dim
+    q_sizes, k_sizes = (batch, sq, shp.q_heads, d), (batch, sq, kv_heads, d)
     _check_cache(cache, batch, kv_heads, d)
     _check_positions(rope, batch, sq)
-    _check(_lib.burst_attn_cache_append(shp, cache, _packed(k, device, batch, sq, kv_heads, d), _packed(v, device, batch, sq, kv_heads, d),
-                                        _numbers(new_rows, device, batch), rope, _packed(q, device, batch, sq, q_heads, d),
-                                        _packed(q_out, device, batch, sq, q_heads, d), stream))
+    _check(_lib.burst_attn_cache_append(shp, cache, _packed(k, device, k_sizes), _packed(v, device, k_sizes),
+                                        _numbers(new_rows, device, batch), rope, _packed(q, device, q_sizes),
+                                        _packed(q_out, device, q_sizes), stream))
 
 
 def burst_attn_decode_workspace_bytes(shp):
@@ -569,14 +571,20 @@ def burst_attn_decode(shp, cache, q, o, lse=None, workspace=None, first_row=None
     stream, device = _current(stream)
     batch, q_heads, kv_heads, d = shp.batch, shp.q_heads, shp.kv_heads, shp.head_dim
     _check_cache(cache, batch, kv_heads, d)
-    _check_device(device, lse, workspace)
+    sizes, ws, n = (batch, 1, q_heads, d), None, 0
     if lse is not None:
+        stride = lse.stride()
         if lse.shape != (batch, q_heads, 1) or lse.dtype != torch.float32:
             raise ValueError(f"lse: fp32 tensor of {(batch, q_heads, 1)} expected")
-        lse = _pack_rowvec(lse.data_ptr(), lse.stride(0), lse.stride(1))
-    ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _check(_lib.burst_attn_decode(shp, cache, _packed(q, device, batch, 1, q_heads, d), _numbers(first_row, device, batch),
-                                  _packed(o, device, batch, 1, q_heads, d), lse, ws, n, stream))
+        if lse.get_device() != device:
+            _check_device(device, lse)
+        lse = _pack_rowvec(lse.data_ptr(), stride[0], stride[1])
+    if workspace is not None:
+        if workspace.get_device() != device:
+            _check_device(device, workspace)
+        ws, n = workspace.data_ptr(), workspace.nbytes
+    _check(_lib.burst_attn_decode(shp, cache, _packed(q, device, sizes), _numbers(first_row, device, batch), _packed(o, device, sizes),
+                                  lse, ws, n, stream))
 
 
 def burst_attn_decode_plan(shp, cache):
