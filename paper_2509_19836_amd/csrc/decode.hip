@@ -37,6 +37,9 @@ typedef const __attribute__((address_space(4))) int32_t* scalar_table;
 constexpr int kTileRows = 32, kDealtWaves = 4;
 constexpr int kDirectWaves = 8;
 constexpr float kStale = 8.f;   // a maximum may fall behind by a factor of 2^8: P, O and their sums stay far inside fp32
+// No part of a weight is 0 (as the second would be of a power of two), or an infinity among the values would give NaN: each is 2^-32 of the weight
+// at least, which stays below what fp32 rounds.  (e4m3 has no infinity.)
+constexpr float kLeastPart = 0x1p-32f;
 constexpr int kCus = 256;
 // Waves that share a SIMD, by the registers that one takes (also: work-groups of four waves that share a CU).
 constexpr int waves_per_simd(int head_dim, bool f8, int nc) { return nc == 2 ? 2 : 2 + (head_dim == 64) + f8; }
@@ -417,7 +420,7 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
       bf16x8 p_part[NC][3];
 #pragma unroll
       for (int nc = 0; nc < NC; ++nc) {
-        float x[8], top = -INFINITY;
+        float x[8], least[8], top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = s[nc][e >> 2][e & 3] * to_log2;
         if (seen != ~0u) {
@@ -440,6 +443,7 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
         for (int e = 0; e < 8; ++e) {
           x[e] = __builtin_amdgcn_exp2f(x[e] - base);
           l[nc] += x[e];
+          least[e] = kLeastPart * x[e];
         }
 #pragma unroll
         for (int part = 0; part < 3; ++part) {
@@ -449,7 +453,10 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
             words[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x[2 * i + 1]), __builtin_bit_cast(uint32_t, x[2 * i]), 0x07060302u);
           p_part[nc][part] = __builtin_bit_cast(bf16x8, words);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[e]) & 0xffff0000u);   // (exact)
+          for (int e = 0; e < 8; ++e) {
+            x[e] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[e]) & 0xffff0000u);   // (exact)
+            if constexpr (!F8) x[e] = fmaxf(x[e], least[e]);
+          }
         }
       }
       // rows that are not seen may hold NaN, which a P of 0 would not silence
