@@ -99,13 +99,16 @@ __device__ __forceinline__ void store16(void* ptr, int64_t off, const SlotPlace&
       store_as<NT>(z, x + (h ? at.hi : at.lo));
     }
   } else {
-    uint8_t* x = (uint8_t*)ptr + off;
+    uint8_t* to = (uint8_t*)ptr + off;
     float z[16];
-    const float over = 1.f / scale;
+    // A scale at either end of fp32, whose reciprocal is no normal number: it and what it divides go by 2^64 towards 1.  (By their exponents: factors
+    // would be multiplied with the reciprocal first.)
+    const int nearer = scale < 0x1p-100f ? 64 : scale > 0x1p100f ? -64 : 0;
+    const float by = __builtin_ldexpf(scale, nearer), over = 1.f / by;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       // y / scale: the product with the reciprocal and what is left of y, as long as that is finite
-      const float near = y[i] * over, s = fabsf(near) < 1e4f ? fmaf(fmaf(-near, scale, y[i]), over, near) : near;
+      const float x = __builtin_ldexpf(y[i], nearer), near = x * over, s = fabsf(near) < 1e4f ? fmaf(fmaf(-near, by, x), over, near) : near;
       z[i] = s != s ? s : fminf(fmaxf(s, -448.f), 448.f);   // (the conversion itself makes NaN of what is too large)
     }
 #pragma unroll
@@ -116,7 +119,7 @@ __device__ __forceinline__ void store16(void* ptr, int64_t off, const SlotPlace&
         int two = __builtin_amdgcn_cvt_pk_fp8_f32(z[8 * h + 4 * w], z[8 * h + 4 * w + 1], 0, false);
         out[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[8 * h + 4 * w + 2], z[8 * h + 4 * w + 3], two, true);
       }
-      *reinterpret_cast<u32x2*>(x + (h ? at.hi : at.lo)) = out;
+      *reinterpret_cast<u32x2*>(to + (h ? at.hi : at.lo)) = out;
     }
   }
 }
