@@ -193,10 +193,10 @@ __device__ __forceinline__ void turn_tensor(const RopeDev& r, const Turn& t, con
 }
 
 template <bool NT>
-__global__ __launch_bounds__(256) void rope_kernel(RopeParams p, TokenShare share) {
+__global__ __launch_bounds__(256) void rope_kernel(RopeParams p, TokenShare share, int32_t first) {
   const int slot = threadIdx.x & ((1 << share.slots_log2) - 1), step = 1 << share.heads_log2;
   const int head = (threadIdx.x >> share.slots_log2) & (step - 1);
-  const int64_t token = (int64_t)blockIdx.x * share.tokens() + (threadIdx.x >> (share.slots_log2 + share.heads_log2));
+  const int64_t token = first + (int64_t)blockIdx.x * share.tokens() + (threadIdx.x >> (share.slots_log2 + share.heads_log2));
   if (token >= (int64_t)p.batch * p.sq) return;
   const int32_t b = (int32_t)token / p.sq, row = (int32_t)token - b * p.sq;   // (batch * sq < 2^31, checked on the host)
   SlotPlace at;
@@ -228,6 +228,19 @@ static TokenShare token_share(int32_t head_dim, int32_t heads, int64_t tokens, b
   return s;
 }
 
+// A launch has fewer than 2^32 threads; more tokens than these are for go to several.
+template <class Params>
+static hipError_t launch_tokens(void (*kernel)(Params, TokenShare, int32_t), const Params& p, TokenShare share, int64_t total, hipStream_t stream) {
+  const int64_t each = (int64_t)share.tokens() << 23;   // 2^31 threads
+  for (int64_t first = 0; first < total; first += each) {
+    const int64_t grid = (std::min(each, total - first) + share.tokens() - 1) / share.tokens();
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(256), 0, stream, p, share, (int32_t)first);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 hipError_t launch_rope(const RopeParams& p, hipStream_t stream) {
   const int64_t total = (int64_t)p.batch * p.sq;
   if (total == 0) return hipSuccess;
@@ -237,18 +250,15 @@ hipError_t launch_rope(const RopeParams& p, hipStream_t stream) {
   const bool f32_to_f32 = (p.q.is_f32 && p.q_out.is_f32) || (p.k.ptr && p.k.is_f32 && p.k_out.is_f32);
   const bool nt = !f32_to_f32 && streams(bytes(p.q, p.q_out, p.q_heads) + bytes(p.k, p.k_out, p.kv_heads), p.head_dim, p.rope);
   const TokenShare share = token_share(p.head_dim, p.q_heads, total, nt && !p.q.is_f32 && 2 * p.kv_heads >= p.q_heads);
-  const int64_t grid = (total + share.tokens() - 1) / share.tokens();
-  if (nt) hipLaunchKernelGGL(rope_kernel<true>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
-  else hipLaunchKernelGGL(rope_kernel<false>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
-  return hipGetLastError();
+  return launch_tokens(nt ? rope_kernel<true> : rope_kernel<false>, p, share, total, stream);
 }
 
 // A token's keys (turned) and values into its row of the cache, and its queries (turned) to q_out.
 template <bool NT>
-__global__ __launch_bounds__(256) void cache_append_kernel(AppendParams p, TokenShare share) {
+__global__ __launch_bounds__(256) void cache_append_kernel(AppendParams p, TokenShare share, int32_t first) {
   const int slot = threadIdx.x & ((1 << share.slots_log2) - 1), step = 1 << share.heads_log2;
   const int head = (threadIdx.x >> share.slots_log2) & (step - 1);
-  const int64_t token = (int64_t)blockIdx.x * share.tokens() + (threadIdx.x >> (share.slots_log2 + share.heads_log2));
+  const int64_t token = first + (int64_t)blockIdx.x * share.tokens() + (threadIdx.x >> (share.slots_log2 + share.heads_log2));
   if (token >= (int64_t)p.batch * p.sq) return;
   const int32_t b = (int32_t)token / p.sq, i = (int32_t)token - b * p.sq;
   int32_t fresh = p.new_rows ? p.new_rows[b] : p.sq;
@@ -281,10 +291,7 @@ hipError_t launch_cache_append(const AppendParams& p, hipStream_t stream) {
   const int64_t bytes = total * p.head_dim * ((p.q.ptr ? 4 * p.q_heads : 0) + 2 * p.kv_heads * (p.cache.is_f8 ? 3 : 4));
   const bool nt = streams(bytes, p.head_dim, p.rope);
   const TokenShare share = token_share(p.head_dim, p.q.ptr ? p.q_heads : p.kv_heads, total, nt && (!p.q.ptr || 2 * p.kv_heads >= p.q_heads));
-  const int64_t grid = (total + share.tokens() - 1) / share.tokens();
-  if (nt) hipLaunchKernelGGL(cache_append_kernel<true>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
-  else hipLaunchKernelGGL(cache_append_kernel<false>, dim3((uint32_t)grid), dim3(256), 0, stream, p, share);
-  return hipGetLastError();
+  return launch_tokens(nt ? cache_append_kernel<true> : cache_append_kernel<false>, p, share, total, stream);
 }
 
 }  // namespace burst

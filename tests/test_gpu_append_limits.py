@@ -33,3 +33,18 @@ def test_scales_of_all_sizes(lib):
         got = P.host[name][page, r]
         assert np.isfinite(got).all(), scales[np.nonzero(~np.isfinite(got))[1]]
         assert (np.abs(got - want) <= tol).all(), scales[np.unique(np.nonzero(np.abs(got - want) > tol)[1])]
+
+
+def test_more_tokens_than_a_launch_has_threads_for(lib):
+    """A padded batch of 3 x 2^28 tokens, few of them new: the rows of a sequence whose tokens two launches share, and of one behind."""
+    import torch
+    d, sq = 128, (1 << 28) - 100
+    P = tp.Paged(lib, np.random.Generator(np.random.PCG64(14)), [20, 150, 30], 16, 1, d)
+    k, v = (torch.randn(3, 1, 1, d, device="cuda").to(torch.bfloat16) for _ in range(2))
+    new = torch.tensor([0, 150, 3], dtype=torch.int32, device="cuda")
+    lib.burst_attn_cache_append(lib.shape(3, 1, 1, d, sq, 0, 1.0), P.cache, k.expand(3, sq, 1, d), v.expand(3, sq, 1, d), new)
+    before = dict(P.host)
+    P.refresh()
+    for name, x in (("k", k), ("v", v)):
+        x = x.double().cpu().numpy()
+        assert np.array_equal(P.host[name], co.append(before[name], np.broadcast_to(x, (3, 150, 1, d)), P.table, [20, 150, 30], [0, 150, 3]))
