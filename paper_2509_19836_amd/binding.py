@@ -475,7 +475,8 @@ def _int32(t, dims):
 def rope(positions, inv_freq, rotary_dim=None, adjacent=False, axis_of_pair=None):
     """A rotation: positions [axes, batch, rows] int32, inv_freq [rotary_dim / 2] fp32, the axis of each pair (default: the first).  A
     plan that a program keeps: it holds the two tensors, whose contents are read when a call that uses it runs."""
-    _check_device(torch.cuda.current_device(), positions, inv_freq)
+    device = torch.cuda.current_device()
+    _check_device(device, positions, inv_freq)
     pairs = inv_freq.numel()
     if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or (rotary_dim is not None and rotary_dim != 2 * pairs):
         raise ValueError("inv_freq: rotary_dim / 2 contiguous fp32 numbers expected")
@@ -486,12 +487,21 @@ def rope(positions, inv_freq, rotary_dim=None, adjacent=False, axis_of_pair=None
         raise ValueError("at most 64 pairs")
     r = burst_rope_t(positions.size(0), 2 * pairs, int(adjacent), 0, inv_freq.data_ptr(), _int32(positions, 3),
                      positions.stride(0), positions.stride(1), (C.c_uint8 * 64)(*axes))
-    r._tensors, r._rows = (positions, inv_freq), tuple(positions.shape[1:])
+    r._tensors, r._rows, r._device = (positions, inv_freq), tuple(positions.shape[1:]), device
     return r
 
 
-def _check_positions(r, batch, sq):
-    if r is not None and r._rows != (batch, sq):
+def _elsewhere(handle, device):
+    """A rotation or a cache is used where its tensors are."""
+    return ValueError(f"made on cuda:{handle._device}, the current device is cuda:{device}")
+
+
+def _check_positions(r, batch, sq, device):
+    if r is None:
+        return
+    if r._device != device:
+        raise _elsewhere(r, device)
+    if r._rows != (batch, sq):
         raise ValueError(f"positions of {batch} sequences of {sq} rows expected, not {r._rows}")
 
 
@@ -500,7 +510,7 @@ def burst_attn_rope(shp, rope, q, q_out, k=None, k_out=None, inverse=False, stre
     stream, device = _current(stream)
     batch, sq, d = shp.batch, shp.sq, shp.head_dim
     q_sizes, k_sizes = (batch, sq, shp.q_heads, d), (batch, sq, shp.kv_heads, d)
-    _check_positions(rope, batch, sq)
+    _check_positions(rope, batch, sq, device)
     _check(_lib.burst_attn_rope(shp, rope, _packed(q, device, q_sizes), _packed(q_out, device, q_sizes), _packed(k, device, k_sizes),
                                 _packed(k_out, device, k_sizes), int(inverse), stream))
 
@@ -508,7 +518,8 @@ def burst_attn_rope(shp, rope, q, q_out, k=None, k_out=None, inverse=False, stre
 def paged_cache(k, v, table, rows, k_scale=None, v_scale=None):
     """A paged cache: k and v [pages, page_rows, kv_heads, head_dim] (bf16 or float8_e4m3fn, in any order of memory), table int32
     [batch, pages of a sequence], rows int32 [batch], scales fp32 [kv_heads].  A handle that a program keeps; it holds the tensors."""
-    _check_device(torch.cuda.current_device(), k, v, table, rows, k_scale, v_scale)
+    device = torch.cuda.current_device()
+    _check_device(device, k, v, table, rows, k_scale, v_scale)
     if k.shape != v.shape or k.dim() != 4 or table.dim() != 2 or rows.dim() != 1 or table.size(0) != rows.size(0):
         raise ValueError("k and v [pages, page_rows, kv_heads, head_dim], table [batch, pages], rows [batch] expected")
     if rows.numel() > 1 and rows.stride(0) != 1:
@@ -518,7 +529,7 @@ def paged_cache(k, v, table, rows, k_scale=None, v_scale=None):
             raise ValueError("scales: kv_heads contiguous fp32 numbers expected")
     c = burst_cache_t(_cache_tensor(k), _cache_tensor(v), k.size(0), k.size(1), table.size(1), _int32(table, 2), table.stride(0),
                       _int32(rows, 1), None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
-    c._tensors, c._sizes = (k, v, table, rows, k_scale, v_scale), (rows.size(0), k.size(2), k.size(3))
+    c._tensors, c._sizes, c._device = (k, v, table, rows, k_scale, v_scale), (rows.size(0), k.size(2), k.size(3)), device
     return c
 
 
@@ -529,7 +540,9 @@ def _cache_tensor(t):
                           t.stride(1), t.stride(2))
 
 
-def _check_cache(cache, batch, kv_heads, d):
+def _check_cache(cache, batch, kv_heads, d, device):
+    if cache._device != device:
+        raise _elsewhere(cache, device)
     if cache._sizes != (batch, kv_heads, d):
         raise ValueError("the cache has another batch, kv_heads or head_dim than the shape")
 
@@ -551,8 +564,8 @@ def burst_attn_cache_append(shp, cache, k, v, new_rows=None, rope=None, q=None, 
     stream, device = _current(stream)
     batch, sq, kv_heads, d = shp.batch, shp.sq, shp.kv_heads, shp.head_dim
     q_sizes, k_sizes = (batch, sq, shp.q_heads, d), (batch, sq, kv_heads, d)
-    _check_cache(cache, batch, kv_heads, d)
-    _check_positions(rope, batch, sq)
+    _check_cache(cache, batch, kv_heads, d, device)
+    _check_positions(rope, batch, sq, device)
     _check(_lib.burst_attn_cache_append(shp, cache, _packed(k, device, k_sizes), _packed(v, device, k_sizes),
                                         _numbers(new_rows, device, batch), rope, _packed(q, device, q_sizes),
                                         _packed(q_out, device, q_sizes), stream))
@@ -570,7 +583,7 @@ def burst_attn_decode(shp, cache, q, o, lse=None, workspace=None, first_row=None
     shp.sk bounds the rows of a sequence; workspace: a one-byte tensor of burst_attn_decode_workspace_bytes(shp) bytes."""
     stream, device = _current(stream)
     batch, q_heads, kv_heads, d = shp.batch, shp.q_heads, shp.kv_heads, shp.head_dim
-    _check_cache(cache, batch, kv_heads, d)
+    _check_cache(cache, batch, kv_heads, d, device)
     sizes, ws, n = (batch, 1, q_heads, d), None, 0
     if lse is not None:
         stride = lse.stride()
