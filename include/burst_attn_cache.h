@@ -3,6 +3,9 @@
  * conventions as burst_attn.h: device pointers owned by the caller, nothing allocated, retained or synchronised, work enqueued
  * on the given stream only, every argument checked on the host before any launch, BURST_OK (0) or a negative burst_status_t.
  *
+ * A chunk may be without rows (sq = 0): burst_attn_rope and burst_attn_cache_append then check what they are given and do nothing, and the pointers of
+ * its tensors and positions may be NULL.
+ *
  * A model turns the queries and keys of a device's chunk by their positions before the ring's attention (burst_attn_rope), and turns
  * the gradients that the backward step leaves in fp32 back again (the same call, inverse).  A sequence that is to be continued keeps its
  * turned keys and its values in pages (burst_attn_cache_append); every further token attends to them (burst_attn_decode).  A cache that is

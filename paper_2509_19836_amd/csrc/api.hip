@@ -48,8 +48,8 @@ int check_shape(const burst_shape_t* s) {
   return BURST_OK;
 }
 
-int check_tensor(const burst_tensor_t* t, int want_dtype_mask /* bit0 bf16 ok, bit1 f32 ok */, TensorDev* out) {
-  if (!t || !t->ptr) return BURST_ERR_INVALID_ARG;
+int check_tensor(const burst_tensor_t* t, int want_dtype_mask /* bit0 bf16 ok, bit1 f32 ok */, TensorDev* out, bool without_memory = false) {
+  if (!t || (!t->ptr && !without_memory)) return BURST_ERR_INVALID_ARG;
   if (t->dtype != BURST_BF16 && t->dtype != BURST_F32) return BURST_ERR_INVALID_ARG;
   if (!((want_dtype_mask >> t->dtype) & 1)) return BURST_ERR_UNSUPPORTED;
   if (((uintptr_t)t->ptr) & 15) return BURST_ERR_INVALID_ARG;
@@ -309,7 +309,8 @@ int check_rope(const burst_rope_t* r, const burst_shape_t* shape, int32_t invers
   if (!r || r->n_axes < 1 || r->n_axes > BURST_ROPE_MAX_AXES) return BURST_ERR_INVALID_ARG;
   if (r->rotary_dim < 1 || r->rotary_dim > shape->head_dim || (r->rotary_dim & 1)) return BURST_ERR_INVALID_ARG;
   if (r->rotary_dim % 16) return BURST_ERR_UNSUPPORTED;   // a thread turns 8 pairs
-  if (!aligned4(r->inv_freq) || !aligned4(r->positions) || r->stride_axis < 0 || r->stride_b < 0) return BURST_ERR_INVALID_ARG;
+  const bool no_rows = shape->sq == 0 && !r->positions;
+  if (!aligned4(r->inv_freq) || !(no_rows || aligned4(r->positions)) || r->stride_axis < 0 || r->stride_b < 0) return BURST_ERR_INVALID_ARG;
   if (r->stride_axis > INT64_MAX / 8 || r->stride_b > (INT64_MAX / 4) / shape->batch) return BURST_ERR_INVALID_ARG;
   for (int i = 0; i < r->rotary_dim / 2; ++i) {
     if (r->axis_of_pair[i] >= r->n_axes) return BURST_ERR_INVALID_ARG;
@@ -326,13 +327,13 @@ int check_rope(const burst_rope_t* r, const burst_shape_t* shape, int32_t invers
   return BURST_OK;
 }
 
-// Input and output of a rotation: one memory, if at all, only as the same tensor.
+// Input and output of a rotation: one memory, if at all, only as the same tensor; none without rows.
 int check_turned(const burst_tensor_t* x, const burst_tensor_t* y, int types_in, int types_out, const burst_shape_t* s, int64_t heads,
                  TensorDev* in, TensorDev* out) {
-  BURST_TRY(check_tensor(x, types_in, in));
-  BURST_TRY(check_tensor(y, types_out, out));
+  BURST_TRY(check_tensor(x, types_in, in, s->sq == 0));
+  BURST_TRY(check_tensor(y, types_out, out, s->sq == 0));
   BURST_TRY(check_no_overlap(*out, s->batch, s->sq, heads, s->head_dim));
-  if (x->ptr == y->ptr && (x->dtype != y->dtype || x->stride_b != y->stride_b || x->stride_s != y->stride_s || x->stride_h != y->stride_h))
+  if (x->ptr && x->ptr == y->ptr && (x->dtype != y->dtype || x->stride_b != y->stride_b || x->stride_s != y->stride_s || x->stride_h != y->stride_h))
     return BURST_ERR_INVALID_ARG;
   return BURST_OK;
 }
@@ -578,7 +579,7 @@ int burst_attn_rope(const burst_shape_t* shape, const burst_rope_t* rope, const 
   BURST_TRY(check_turned(q, q_out, 3, 3, shape, shape->q_heads, &p.q, &p.q_out));
   if ((k == nullptr) != (k_out == nullptr)) return BURST_ERR_INVALID_ARG;
   if (k) BURST_TRY(check_turned(k, k_out, 3, 3, shape, shape->kv_heads, &p.k, &p.k_out));
-  if (k && k_out->ptr == q_out->ptr) return BURST_ERR_INVALID_ARG;
+  if (k && k_out->ptr && k_out->ptr == q_out->ptr) return BURST_ERR_INVALID_ARG;
   if (shape->sq > kMaxTokens / shape->batch) return BURST_ERR_UNSUPPORTED;
   p.batch = shape->batch;
   p.sq = (int32_t)shape->sq;
@@ -600,8 +601,8 @@ int burst_attn_cache_append(const burst_shape_t* shape, const burst_cache_t* cac
   const TensorDev pages{p.cache.k, p.cache.s_page, p.cache.s_row, p.cache.s_head, 0};
   BURST_TRY(check_no_overlap(pages, p.cache.n_pages, p.cache.page_rows, shape->kv_heads, shape->head_dim));
   if (p.cache.k == p.cache.v) return BURST_ERR_INVALID_ARG;
-  BURST_TRY(check_tensor(k, 1, &p.k));
-  BURST_TRY(check_tensor(v, 1, &p.v));
+  BURST_TRY(check_tensor(k, 1, &p.k, shape->sq == 0));
+  BURST_TRY(check_tensor(v, 1, &p.v, shape->sq == 0));
   if (new_rows && !aligned4(new_rows)) return BURST_ERR_INVALID_ARG;
   if (rope) BURST_TRY(check_rope(rope, shape, 0, &p.rope));
   if ((q == nullptr) != (q_out == nullptr)) return BURST_ERR_INVALID_ARG;
