@@ -527,7 +527,8 @@ def paged_cache(k, v, table, rows, k_scale=None, v_scale=None):
     for s in (k_scale, v_scale):
         if s is not None and (s.dtype != torch.float32 or not s.is_contiguous() or s.numel() != k.size(2)):
             raise ValueError("scales: kv_heads contiguous fp32 numbers expected")
-    c = burst_cache_t(_cache_tensor(k), _cache_tensor(v), k.size(0), k.size(1), table.size(1), _int32(table, 2), table.stride(0),
+    c = burst_cache_t(_cache_tensor(k), _cache_tensor(v), k.size(0), k.size(1), table.size(1), _int32(table, 2),
+                      table.stride(0) if table.size(0) > 1 else 0,
                       _int32(rows, 1), None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
     c._tensors, c._sizes, c._device = (k, v, table, rows, k_scale, v_scale), (rows.size(0), k.size(2), k.size(3)), device
     return c

@@ -82,3 +82,16 @@ def _cache_on_device_1(lib):
         x.dim, x.size, x.numel = t.dim, t.size, t.numel
         numbers.append(x)
     return lib.paged_cache(pages, pages, *numbers)
+
+
+def test_a_table_of_one_sequence_has_any_stride(lib, monkeypatch):
+    """A dimension of one entry: whatever its stride is (1 here, as a column of a larger table turned round), no row of the table is skipped."""
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    pages = torch.zeros(3, 16, 2, 64, dtype=torch.bfloat16)
+    table = torch.zeros(5, 1, dtype=torch.int32).t()
+    assert table.shape == (1, 5) and table.stride() == (1, 1)
+    cache = lib.paged_cache(pages, torch.zeros_like(pages), table, torch.zeros(1, dtype=torch.int32))
+    assert lib.burst_attn_decode_plan(lib.shape(1, 2, 2, 64, 1, 80, 1.0), cache)[2]
+    two = torch.zeros(2, 9, dtype=torch.int32)[:, :5]
+    assert lib.paged_cache(pages, torch.zeros_like(pages), two, torch.zeros(2, dtype=torch.int32)).table_stride == 9
