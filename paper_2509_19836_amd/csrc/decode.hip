@@ -31,15 +31,16 @@ namespace burst {
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 // Read by scalar loads: a vector load of a page's number would have to be waited for together with all tiles asked for before it.
 typedef const __attribute__((address_space(4))) int32_t* scalar_table;
 
 constexpr int kTileRows = 32, kDealtWaves = 4;
 constexpr int kDirectWaves = 8;
 constexpr float kStale = 8.f;   // a maximum may fall behind by a factor of 2^8: P, O and their sums stay far inside fp32
-// No part of a weight is 0 (as the second would be of a power of two), or an infinity among the values would give NaN: each is 2^-32 of the weight
-// at least, which stays below what fp32 rounds.  (e4m3 has no infinity.)
-constexpr float kLeastPart = 0x1p-32f;
+// No part of a weight is 0 (as the second would be of a power of two), or an infinity among the values would give NaN: each is about 2^-32 of the
+// weight at least, which stays below what fp32 rounds.  (e4m3 has no infinity.)  In bits of bf16, which grow with the number:
+constexpr uint16_t kLeastPart = 32 << 7;
 constexpr int kCus = 256;
 // Waves that share a SIMD, by the registers that one takes (also: work-groups of four waves that share a CU).
 constexpr int waves_per_simd(int head_dim, bool f8, int nc) { return nc == 2 ? 2 : 2 + (head_dim == 64) + f8; }
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
       bf16x8 p_part[NC][3];
 #pragma unroll
       for (int nc = 0; nc < NC; ++nc) {
-        float x[8], least[8], top = -INFINITY;
+        float x[8], top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = s[nc][e >> 2][e & 3] * to_log2;
         if (seen != ~0u) {
@@ -443,20 +444,22 @@ __global__ __launch_bounds__(DIRECT ? 64 * kDirectWaves : 64 * kDealtWaves, wave
         for (int e = 0; e < 8; ++e) {
           x[e] = __builtin_amdgcn_exp2f(x[e] - base);
           l[nc] += x[e];
-          least[e] = kLeastPart * x[e];
         }
+        u16x2 least[4];
 #pragma unroll
         for (int part = 0; part < 3; ++part) {
           u32x4 words;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            words[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x[2 * i + 1]), __builtin_bit_cast(uint32_t, x[2 * i]), 0x07060302u);
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t two = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x[2 * i + 1]), __builtin_bit_cast(uint32_t, x[2 * i]), 0x07060302u);
+            u16x2 bits2 = __builtin_bit_cast(u16x2, two);   // (of words[i] itself the bit cast would take the vector's first word)
+            if (!F8 && part == 0) least[i] = __builtin_elementwise_sub_sat(bits2, u16x2{kLeastPart, kLeastPart});
+            if (!F8 && part != 0) bits2 = __builtin_elementwise_max(bits2, least[i]);
+            words[i] = __builtin_bit_cast(uint32_t, bits2);
+          }
           p_part[nc][part] = __builtin_bit_cast(bf16x8, words);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x[e] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[e]) & 0xffff0000u);   // (exact)
-            if constexpr (!F8) x[e] = fmaxf(x[e], least[e]);
-          }
+          for (int e = 0; e < 8; ++e) x[e] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[e]) & 0xffff0000u);   // (exact)
         }
       }
       // rows that are not seen may hold NaN, which a P of 0 would not silence
