@@ -36,7 +36,8 @@ extern "C" {
  *   rotary_dim  : a positive multiple of 16, at most head_dim (0 < rotary_dim: INVALID_ARG otherwise; not a multiple of 16: UNSUPPORTED).
  *   inv_freq    : fp32 [rotary_dim / 2], device; any values.
  *   positions   : int32 [n_axes][batch][rows], device, rows contiguous, strides in elements (0 broadcasts); any values, negative too.
- * Angles are formed in 64 bits, so that far positions keep their place on the circle; sine and cosine are exact to 1e-7.
+ * Angles are formed in 64 bits, by three roundings, so that far positions keep their place on the circle: sine and cosine are off by at most
+ * 2^-24 + 3 * 2^-53 |a| (a in radians: 1e-7 up to 10^8, 8e-7 at position 2^31 with frequency 1; without meaning from 10^15 on).
  */
 typedef struct {
   int32_t n_axes;     /* 1 .. BURST_ROPE_MAX_AXES */

@@ -20,9 +20,12 @@
 //   us, one and a half times as many 212 -> 232, twice as many 228.  Two tiles under way in a wave instead of one: no gain (the
 //   CU's own rate of loads, about 50 GB/s, is what a short sequence waits for, and the memory a long one).
 //
-// Measured (rows x key heads, a cache of its own for each of three calls in turn): 131072 x 32 bf16 319 us, 6.73 TB/s (a copy reaches 5.2, a
+// Measured (rows x key heads, a cache of its own for each of three calls in turn): 131072 x 32 bf16 320 us, 6.72 TB/s (a copy reaches 5.2, a
 // fill 6.9); 32 sequences of 32768 and fewer x 8 in e4m3 135 us, 5.3 TB/s (128-byte rows of heads side by side; head by head 5.7); 64
-// of 4096 and fewer x 8 64 us, 5.1 TB/s; 32768 x 8 32 us, 4.2 TB/s, of which 5 us are the second kernel and 6 the first loads.
+// of 4096 and fewer x 8 65 us, 5.1 TB/s; 32768 x 8 32 us, 4.2 TB/s, of which 5 us are the second kernel and 6 the first loads.
+// Pages of a multiple of 16 rows, whose size else does not matter, against others (65536 x 8, heads side by side; a row's address by each lane and a
+// shuffle): bf16 54 us and 58-62, e4m3 40 and 42-45; direct, 16 sequences of 1000 x 8, 20.8 and 24.9.  Query heads over a key head (4 x 131072 x 1 of 128,
+// floor 52 us): 1 to 16 51-53 us, 17 to 32 (queries in LDS) 56-59, 33 to 64 98-101, as every 32 read the keys and values for themselves.
 #include "cache.hpp"
 #include "kernels.hpp"
 #include "mfma16.hpp"

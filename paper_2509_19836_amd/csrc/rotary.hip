@@ -18,7 +18,8 @@ struct Turn {
 };
 
 // Sine and cosine of a thread's 8 pairs at one token, rounded to fp32 once.  The angle in whole turns, position * inv_freq / 2 pi, is
-// formed in 64 bits: 2^31 positions leave 1e-7 of a turn, where 32 bits would lose the place on the circle from about 10^5 on.
+// formed in 64 bits by three roundings, off by 3 * 2^-53 of itself: 7e-7 radians at position 2^31 with frequency 1, where 32 bits would lose the
+// place on the circle from about 10^5 on.
 // What is left of it after the whole turns, and then after the quarter turns, is within +-pi / 4, where the Taylor series of sine to
 // x^11 and cosine to x^10 are off by less than 1e-11 and 2e-10.
 __device__ __forceinline__ void turn_of(const RopeDev& r, int slot, int32_t b, int32_t row, Turn& t) {

@@ -12,7 +12,8 @@ from . import binding as lib
 
 class PagedCache:
     """Pages of page_rows rows for `batch` sequences of up to max_rows rows each on the current device: bf16, or float8_e4m3fn over scales
-    of the key heads.  In memory a page has its rows head by head, the order that is read fastest."""
+    of the key heads.  In memory a page has its rows head by head, the order that is read fastest.  The keys and values are one layer's; another
+    layer's, in tensors of the same n_pages and page_rows, go by the same numbers: binding.paged_cache(k, v, cache.table, cache.rows)."""
 
     def __init__(self, n_pages, page_rows, batch, kv_heads, head_dim, max_rows, dtype=torch.bfloat16, k_scale=None, v_scale=None):
         device = torch.device("cuda", torch.cuda.current_device())
@@ -27,8 +28,9 @@ class PagedCache:
         self.handle = lib.paged_cache(k, v, self.table, self.rows, k_scale, v_scale)
 
     def grow(self, new_rows):
-        """Room for new_rows[b] more rows of each sequence, which count from now on: the next append fills them (in every layer that shares
-        the table), on the current stream.  Raises, and changes nothing, where pages run out or a sequence would pass max_rows."""
+        """Room for new_rows[b] more rows of each sequence, which count from now on: the next append (in every layer that goes by the table) fills
+        them, on the current stream, for which the host waits here.  Raises, and changes nothing, where pages run out or a sequence would
+        pass max_rows."""
         lengths = [n + m for n, m in zip(self.lengths, new_rows, strict=True)]
         if min(new_rows) < 0 or max(lengths) > self.max_rows:
             raise ValueError(f"a sequence has 0 to {self.max_rows} rows")
@@ -68,7 +70,9 @@ def workspace(cache, q_heads):
 
 
 def attend(cache, q, scale, o, lse, ws, first_row=None, stream=None):
-    """One new token of each sequence, q [batch, 1, q_heads, head_dim] as append left it, over all rows of the cache: o, lse."""
+    """One new token of each sequence, q [batch, 1, q_heads, head_dim] as append left it, over all rows of the cache: o, lse.  The call's bound
+    of the rows is max_rows, whatever the sequences have, so that a captured one serves them as they grow; a program that knows less to be enough
+    calls binding.burst_attn_decode with that, which is faster for short sequences in a large cache."""
     B, _, Hq, d = q.shape
     shp = lib.shape(B, Hq, cache.handle._tensors[0].shape[2], d, 1, cache.max_rows, scale)
     lib.burst_attn_decode(shp, cache.handle, q, o, lse, ws, first_row=first_row, stream=stream)
