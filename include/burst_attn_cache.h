@@ -106,7 +106,7 @@ int burst_attn_cache_append(const burst_shape_t* shape, const burst_cache_t* cac
  * the bound; but a bound that keeps all keys and values of a head within 256 KiB (512 with 256 (sequence, key head) pairs and more) makes the call
  * one launch instead of two.  O is exact to fp32 rounding before it is cast: the numbers
  * exp(S - Lse) are multiplied in the three bf16 parts that their 24 bits are.  An infinity among the values that are seen is its element of O
- * for every query head whose weight there is 2^-90 of the largest or more; below that, and where infinities of both signs meet, the element is NaN.  A row's result depends on the other sequences of the batch by roundings in fp32 alone.
+ * for every query head whose weight there is 2^-90 of the largest or more (below that it may be NaN, as it is where infinities of both signs meet).  A row's result depends on the other sequences of the batch by roundings in fp32 alone.
  * Rows that are not seen may hold anything, NaN too.  o and lse share memory with nothing that the call reads.
  * workspace: burst_attn_decode_workspace_bytes(shape) bytes, 256-byte aligned, contents on entry irrelevant, on return unspecified; calls
  * that share one must be ordered on one stream.  The size depends on batch, the heads, head_dim and sk; it is 0 for some shapes, for which

@@ -71,3 +71,22 @@ def test_rows_without_weight_have_no_share(lib, mode):
         P.host["k"][page, r] = 0.0
     size = P.decode(q_host, 128 ** -0.5)[3]                                 # the tolerance goes by the scores of the others
     tp.check_decode(o, lse, (O, lse_ref, weight, size), 333, 128)
+
+
+@pytest.mark.parametrize("place", [0, 250, 399])
+@pytest.mark.parametrize("mode", list(MODES))
+def test_infinite_values_of_small_weight(lib, mode, place):
+    """A weight of 2^-86 of the others', before them, among them and behind them: the infinity is there all the same."""
+    rng = np.random.Generator(np.random.PCG64(wl.BASE_SEED + 90060 + place))
+    Hkv, bound = MODES[mode][0], bound_of(mode, 16)
+    P = tp.Paged(lib, rng, [400], 16, Hkv, 64, cols=bound // 16)
+    P.dev["k"].zero_()
+    page, r = co.slots(P.table, 16, 0, place)
+    P.dev["k"][page, r, :, 11] = -60.0                                      # (e^-60 = 2^-86.6)
+    P.dev["v"][page, r, :, 3], P.dev["v"][page, r, :, 9] = math.inf, -math.inf
+    q, _ = tp.queries(rng, 1, 3 * Hkv, 64)
+    q[..., 11] = 1.0
+    o, lse = tp.run_decode(lib, P, q, 1.0, bound)
+    assert (o[..., 3] == math.inf).all() and (o[..., 9] == -math.inf).all()
+    o[..., [3, 9]] = 0.0
+    assert o.isfinite().all() and np.abs(lse.cpu().numpy() - math.log(399)).max() <= 1e-5
