@@ -1,5 +1,6 @@
 /*
- * libburstattn -- rotary positions, a paged key-value cache, and the attention of one new token over it.  Same library, same
+ * libburstattn -- rotary positions, a paged key-value cache, the attention of one new token or of a tree of drafted ones over it, and
+ * pages and rows of the cache copied.  Same library, same
  * conventions as burst_attn.h: device pointers owned by the caller, nothing allocated, retained or synchronised, work enqueued
  * on the given stream only, every argument checked on the host before any launch, BURST_OK (0) or a negative burst_status_t.
  *
@@ -10,6 +11,9 @@
  * the gradients that the backward step leaves in fp32 back again (the same call, inverse).  A sequence that is to be continued keeps its
  * turned keys and its values in pages (burst_attn_cache_append); every further token attends to them (burst_attn_decode).  A cache that is
  * sharded over the devices of a ring is decoded by each device over its own rows; burst_attn_lse_merge joins the (O, Lse) pairs.
+ * Where several next tokens were guessed they are appended together, attend to the cache and to each other as their tree says (burst_attn_tree), and the
+ * rows of those that turn out right are moved to the front (burst_attn_cache_keep_rows).  A sequence that is continued in several ways shares its full
+ * pages through the table and has its last one copied (burst_attn_cache_copy_pages).
  */
 #ifndef BURST_ATTN_CACHE_H
 #define BURST_ATTN_CACHE_H
@@ -115,6 +119,68 @@ int burst_attn_cache_append(const burst_shape_t* shape, const burst_cache_t* cac
 int64_t burst_attn_decode_workspace_bytes(const burst_shape_t* shape);   /* host only; -1 for an invalid shape */
 int burst_attn_decode(const burst_shape_t* shape, const burst_cache_t* cache, const burst_tensor_t* q, const int32_t* first_row,
                       const burst_tensor_t* o, const burst_rowvec_t* lse, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+#define BURST_TREE_MAX_TOKENS 64
+
+/*
+ * What new tokens see of a cache.  Sequence b has tokens[b] of them (device int32 [batch], 0 .. sq, a number outside is taken as the nearest; NULL: sq
+ * for all).  Their own rows are the last tokens[b] ones of its rows[b], as an append leaves them; the rows before those are older.
+ *   seen      : device, a word of 64 bits for each token, [batch][sq] (stride in words, 0: one tree for all): token i sees new token j iff bit j is
+ *               set; bits of tokens that are not there are not looked at.  A token sees itself by its own bit.  NULL: a chain, i sees 0 .. i.
+ *   first_row : device int32 [batch][sq] (stride in numbers, 0 broadcasts): token i sees of the older rows those from first_row on and, whatever it says, the
+ *               first sink_rows ones of the sequence.  Any number; NULL: 0, all of them.  (A sliding window of w tokens is first_row = position - w + 1;
+ *               new tokens are hidden by their bits alone.)
+ *   elsewhere : != 0: the new tokens' own rows are not in this cache (a ring's devices but one): every row here is older, seen is not looked at.
+ */
+typedef struct {
+  const uint64_t* seen;
+  int64_t seen_stride;
+  const int32_t* first_row;
+  int64_t first_stride;
+  const int32_t* tokens;
+  int32_t sink_rows;   /* >= 0 */
+  int32_t elsewhere;
+} burst_tree_t;
+
+/*
+ * Attention of a few new tokens of every sequence over its rows in the cache, each over the rows t that it sees, as a step of the ring gives it:
+ *     S_t = scale * q . K_t;  Lse = log sum exp S_t (natural log);  O = sum exp(S_t - Lse) V_t;   without a row O = 0, Lse = -inf.
+ * q is bf16 [batch, sq, q_heads, head_dim], o bf16 or fp32 of that shape, lse [batch, q_heads, sq], or NULL: not wanted.  Tokens behind a sequence's last
+ * one (padding) are not read, and their rows of o and lse are left as they were.
+ * shape: sq is 1 .. BURST_TREE_MAX_TOKENS (more: UNSUPPORTED; a longer chain goes by several calls, each behind its append); sk is a bound on every
+ * sequence's rows, the new ones among them, at most table_cols * page_rows (INVALID_ARG): rows at and behind it are not seen.  batch * q_heads * sq above 2^25, or
+ * batch * sk of about 2^36 and more: UNSUPPORTED.
+ * O in fp32 is exact to fp32 rounding: the numbers exp(S - Lse) are multiplied in the three bf16 parts that their 24 bits are.  For O in bf16 they may be rounded to
+ * 16 bits (2^-17 of each), far below the cast.  A row that is seen by none of a sequence's tokens, or that has no page, may hold anything, NaN too.  An infinity or NaN in a
+ * row that one of them sees reaches those that see it, and may reach the sequence's other tokens.  A token's result depends on the other tokens and sequences by
+ * roundings in fp32 alone.  o and lse share memory with nothing that the call reads.
+ * workspace: burst_attn_tree_workspace_bytes(shape) bytes, 256-byte aligned, contents on entry irrelevant, on return unspecified; calls that share one must be
+ * ordered on one stream.  The size depends on batch, sq, the heads, head_dim and sk; it is 0 for some shapes, for which workspace may be NULL.
+ */
+int64_t burst_attn_tree_workspace_bytes(const burst_shape_t* shape);   /* host only; -1 for an invalid shape */
+int burst_attn_tree(const burst_shape_t* shape, const burst_cache_t* cache, const burst_tree_t* tree, const burst_tensor_t* q, const burst_tensor_t* o,
+                    const burst_rowvec_t* lse, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * The first rows of pages copied to other pages, in n_layers caches (at most BURST_CACHE_MAX_LAYERS, in as few launches as they allow) that are alike
+ * but for where k and v lie: types, strides, n_pages, page_rows (INVALID_ARG otherwise; table, rows and scales are not looked at).  moves: device
+ * int32 [n_moves][3]: from, to, and the number of rows (a number outside 0 .. page_rows is taken as the nearest).  A move from or to what is no page does nothing, nor does one
+ * from a page to itself.  No page may be the destination of two moves that are carried out, or of one and the source of another.  shape: kv_heads and head_dim are read.
+ */
+#define BURST_CACHE_MAX_LAYERS 1024
+int burst_attn_cache_copy_pages(const burst_shape_t* shape, int32_t n_layers, const burst_cache_t* caches, const int32_t* moves, int64_t n_moves,
+                                void* hip_stream);
+
+/*
+ * Of each sequence's last new_rows[b] rows (device int32 [batch], 0 .. sq, a number outside is taken as the nearest; NULL: sq) those that stay, moved to the
+ * front of them, in n_layers caches as above, which also share one table and its rows: for i < kept[b] (device int32 [batch], taken as at most new_rows[b]) row i of them
+ * becomes what row from[b][i] of them was before the call (device int32 [batch][sq], stride in numbers, 0 broadcasts).  A row may be named more than once, in
+ * any order; where from is outside 0 .. new_rows[b] - 1, or either row has no page, the row stays as it is, and so do rows from kept[b] on.  rows itself
+ * is not changed: the program takes new_rows[b] - kept[b] off it afterwards.  No two of the rows may be one row of a page.
+ * shape: batch, kv_heads, head_dim and sq are read; sq is at most BURST_TREE_MAX_TOKENS (UNSUPPORTED).
+ */
+int burst_attn_cache_keep_rows(const burst_shape_t* shape, int32_t n_layers, const burst_cache_t* caches, const int32_t* from, int64_t from_stride,
+                               const int32_t* new_rows, const int32_t* kept, void* hip_stream);
 
 #ifdef __cplusplus
 }

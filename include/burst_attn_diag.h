@@ -82,6 +82,13 @@ int burst_lm_head_tile_plan(const burst_lm_head_shape_t* shape, int32_t out[6]);
  * Host only; nothing of the cache is read but its type, head stride and page size. */
 int burst_attn_decode_plan(const burst_shape_t* shape, const burst_cache_t* cache, int32_t out[3]);
 
+/* The same of a burst_attn_tree: out[0] shares, each a work-group for every key head and every out[1] columns (new tokens times query heads of a key
+ * head); out[2] = 1: no dealing, a share for every sequence.  Host only. */
+int burst_attn_tree_plan(const burst_shape_t* shape, int32_t out[3]);
+
+/* How a burst_lm_head_scores is dealt: out[0] waves of a work-group that take a row's part together, out[1] such parts of a row.  Host only. */
+int burst_lm_head_scores_plan(const burst_scores_shape_t* shape, int32_t out[2]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -90,6 +90,43 @@ int burst_lm_head_loss_noalloc(const burst_lm_head_shape_t* shape, const void* h
                                void* d_h, int32_t d_h_dtype, int64_t ld_dh, float* d_w, int64_t ld_dw,
                                int32_t accumulate_dw, void* hip_stream);
 
+/*
+ * Scores of tokens from logits that the program has (of drafted or generated tokens, of a prompt, of answers that are trained on).  With
+ * x = scale * logits (scale: 1 / temperature):
+ *   lse_i = log sum_j exp x_ij;  logp_i = x_i,y_i - lse_i;  entropy_i = - sum_j p_ij log p_ij,  p_ij = exp(x_ij - lse_i);
+ *   top_ids_i: the n_top words of the largest logits, the largest first, among equal ones (0 and -0 are) the lowest index first; top_logp_i their log probabilities.
+ *   logits : [n_tokens][ld], BURST_BF16 or BURST_F32, 16-byte aligned, ld >= vocab, any number (rows that are multiples of 16 bytes are read a little faster).
+ *   y      : int64 [n_tokens]; a word outside [0, vocab) marks an ignored token: logp 0.  NULL with logp == NULL.
+ *   logp, lse, entropy : fp32 [n_tokens], each NULL if not wanted.  top_logp fp32, top_ids int64 : [n_tokens][n_top], each NULL if not wanted.
+ * Words at -inf (masked ones) have no share; where all are, lse = logp = top_logp = -inf and entropy = 0.  A NaN or +inf among a token's logits makes its scores NaN; with a NaN
+ * its top_ids are words, but no particular ones.
+ * workspace: burst_lm_head_scores_workspace_bytes(shape) bytes, 256-byte aligned, or NULL where that is 0; contents on entry irrelevant; calls that share one must be ordered
+ * on one stream.  With n_tokens = 0 pointers are not looked at.
+ * Errors: INVALID_ARG; UNSUPPORTED beyond 64 n_top, 2^30 words or 2^25 tokens.
+ */
+#define BURST_SCORES_MAX_TOP 64
+typedef struct {
+  int64_t n_tokens;   /* >= 0 */
+  int64_t vocab;      /* >= 1 */
+  int32_t n_top;      /* 0 .. 64, at most vocab */
+  float scale;        /* positive, finite */
+} burst_scores_shape_t;
+
+int64_t burst_lm_head_scores_workspace_bytes(const burst_scores_shape_t* shape);   /* host only; -1 for an invalid shape */
+int burst_lm_head_scores(const burst_scores_shape_t* shape, const void* logits, int32_t logits_dtype, int64_t ld, const int64_t* y, float* logp, float* lse,
+                         float* entropy, float* top_logp, int64_t* top_ids, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * The gradient of the logits from those of the scores (fp32, of the shapes above, each NULL if there is none, not all of them):
+ *   d_logits_ij = scale * ( p_ij (g_lse_i - g_logp_i - sum_k g_top_ik - g_entropy_i (log p_ij + entropy_i)) + g_logp_i [j = y_i] + sum_k g_top_ik [j = top_ids_ik] )
+ * lse, and entropy with g_entropy, are those that burst_lm_head_scores gave; y comes with g_logp, top_ids with g_top.  A word outside [0, vocab) takes its gradient with it, among
+ * top_ids too; one that is named several times gets the sum.  Where lse is -inf the gradient is 0.  d_logits: [n_tokens][ld_d], bf16 or fp32, overwritten
+ * (words 0 .. vocab - 1 of each row); it may be logits itself (same type and ld), else they share no memory.
+ */
+int burst_lm_head_scores_bwd(const burst_scores_shape_t* shape, const void* logits, int32_t logits_dtype, int64_t ld, const int64_t* y, const float* lse,
+                             const float* entropy, const int64_t* top_ids, const float* g_logp, const float* g_lse, const float* g_entropy, const float* g_top,
+                             void* d_logits, int32_t d_logits_dtype, int64_t ld_d, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -93,3 +93,76 @@ def decode(q, k, v, table, rows, scale, first=None, max_rows=None, k_scale=None,
             weight[b, h] = p @ np.abs(V[:, h // group]) / p.sum()
             size[b, h] = (np.abs(K[:, h // group]) @ np.abs(q[b, h].astype(np.float64))).max() * scale
     return O, lse, weight, size
+
+
+def tree_visible(n_tokens, rows, bound, seen=None, first=None, sinks=0, elsewhere=False):
+    """[tokens, rows] which rows of a sequence its new tokens see: seen a list of words, first a list of numbers; rows below the bound alone."""
+    older = rows if elsewhere else rows - n_tokens
+    vis = np.zeros((n_tokens, max(rows, 0)), bool)
+    for i in range(n_tokens):
+        for t in range(min(rows, bound)):
+            if t < older:
+                vis[i, t] = t < sinks or first is None or t >= first[i]
+            else:
+                j = t - older
+                vis[i, t] = j <= i if seen is None else bool((int(seen[i]) >> j) & 1)
+    return vis
+
+
+def tree(q, k, v, table, rows, tokens, scale, seen=None, first=None, sinks=0, elsewhere=False, max_rows=None, k_scale=None, v_scale=None):
+    """q [batch, sq, q_heads, head_dim], sequence b's first tokens[b] of them, over the cache: O [batch, sq, q_heads, head_dim], Lse [batch, q_heads, sq], and for
+    tolerances the sum of P |V| and the largest sum of |q| |K|, of the tokens that are there (NaN elsewhere)."""
+    B, sq, Hq, d = q.shape
+    n_pages, page_rows, Hkv, _ = k.shape
+    group = Hq // Hkv
+    ks = np.ones(Hkv) if k_scale is None else np.asarray(k_scale, np.float64)
+    vs = np.ones(Hkv) if v_scale is None else np.asarray(v_scale, np.float64)
+    O, weight = np.full((B, sq, Hq, d), np.nan), np.full((B, sq, Hq, d), np.nan)
+    lse, size = np.full((B, Hq, sq), np.nan), np.full((B, Hq, sq), np.nan)
+    for b in range(B):
+        n = min(max(int(tokens[b]), 0), sq)
+        have = min(max(int(rows[b]), 0), table.shape[1] * page_rows)
+        vis = tree_visible(n, have, have if max_rows is None else max_rows, None if seen is None else seen[b], None if first is None else first[b], sinks,
+                           elsewhere)
+        page, r = slots(table, page_rows, b, np.arange(have))
+        vis &= (page >= 0) & (page < n_pages)
+        for i in range(n):
+            at = np.flatnonzero(vis[i])
+            K = k[page[at], r[at]].astype(np.float64) * ks[:, None]
+            V = v[page[at], r[at]].astype(np.float64) * vs[:, None]
+            for h in range(Hq):
+                O[b, i, h], weight[b, i, h], lse[b, h, i], size[b, h, i] = 0, 0, -np.inf, 0
+                if at.size == 0:
+                    continue
+                s = K[:, h // group] @ q[b, i, h].astype(np.float64) * scale
+                p = np.exp(s - s.max())
+                lse[b, h, i] = s.max() + np.log(p.sum())
+                O[b, i, h] = p @ V[:, h // group] / p.sum()
+                weight[b, i, h] = p @ np.abs(V[:, h // group]) / p.sum()
+                size[b, h, i] = (np.abs(K[:, h // group]) @ np.abs(q[b, i, h].astype(np.float64))).max() * scale
+    return O, lse, weight, size
+
+
+def copy_pages(cache, moves):
+    """cache [pages, page_rows, ...] after all moves (from, to, rows)."""
+    out = np.array(cache)
+    for source, to, rows in np.asarray(moves).tolist():
+        if 0 <= source < cache.shape[0] and 0 <= to < cache.shape[0]:
+            out[to, :max(rows, 0)] = cache[source, :max(rows, 0)]
+    return out
+
+
+def keep_rows(cache, table, rows, source, new, kept):
+    """cache [pages, page_rows, ...] with new row source[b][i] of every sequence b, as it was, in the place of its new row i < kept[b]."""
+    out, n_pages, page_rows = np.array(cache), cache.shape[0], cache.shape[1]
+    sq, most = np.asarray(source).shape[1], np.asarray(table).shape[1] * page_rows
+    for b in range(len(rows)):
+        have, n = min(max(int(rows[b]), 0), most), min(max(int(new[b]), 0), sq)
+        for i in range(min(int(kept[b]), n)):
+            j = int(source[b][i])
+            if not 0 <= j < n or have - n + min(i, j) < 0:
+                continue
+            (p0, r0), (p1, r1) = slots(table, page_rows, b, have - n + j), slots(table, page_rows, b, have - n + i)
+            if 0 <= p0 < n_pages and 0 <= p1 < n_pages:
+                out[p1, r1] = cache[p0, r0]
+    return out

@@ -95,3 +95,54 @@ def lm_head_loss_tiled(H, W, Y, B_s, B_v, grad_scale=1.0):
             dH[s0:s1] += G @ W_j
             dW[v0:v1] += G.T @ H_i
     return loss, lse_all, dH, dW
+
+
+def scores(logits, y=None, n_top=0, scale=1.0):
+    """Scores of tokens from logits [n, vocab]: a dict of logp (with y; 0 for a word outside), lse, entropy, top_logp and top_ids."""
+    x = np.asarray(logits, np.float64) * scale
+    n, v = x.shape
+    out = {"lse": np.full(n, -np.inf), "entropy": np.zeros(n), "top_logp": np.full((n, n_top), -np.inf), "top_ids": np.zeros((n, n_top), np.int64)}
+    logp = np.full((n, v), -np.inf)
+    for i in range(n):
+        top = x[i].max()
+        if top > -np.inf:
+            out["lse"][i] = top + np.log(np.exp(x[i] - top).sum())
+            logp[i] = x[i] - out["lse"][i]
+            here = logp[i] > -np.inf
+            out["entropy"][i] = -(np.exp(logp[i][here]) * logp[i][here]).sum()
+        order = sorted(range(v), key=lambda j: (-logits[i, j], j))[:n_top]
+        out["top_ids"][i], out["top_logp"][i] = order, logp[i, order]
+    if y is not None:
+        inside = (np.asarray(y) >= 0) & (np.asarray(y) < v)
+        out["logp"] = np.where(inside, logp[np.arange(n), np.where(inside, y, 0)], 0.0)
+    return out
+
+
+def scores_bwd(logits, y=None, top_ids=None, g_logp=None, g_lse=None, g_entropy=None, g_top=None, scale=1.0):
+    """The gradient of the logits, score by score: that of log p_j is e_j - p, of lse p, of the entropy -p (log p + entropy)."""
+    x = np.asarray(logits, np.float64) * scale
+    n, v = x.shape
+    s = scores(logits, scale=scale)
+    out = np.zeros((n, v))
+    for i in range(n):
+        if s["lse"][i] == -np.inf:
+            continue
+        p = np.exp(x[i] - s["lse"][i])
+
+        def of_word(j):
+            g = -p
+            g[j] += 1.0
+            return g
+
+        if g_lse is not None:
+            out[i] += g_lse[i] * p
+        if g_logp is not None and 0 <= y[i] < v:
+            out[i] += g_logp[i] * of_word(int(y[i]))
+        if g_entropy is not None:
+            logp = np.where(p > 0, x[i] - s["lse"][i], 0.0)
+            out[i] -= g_entropy[i] * p * (logp + s["entropy"][i])
+        if g_top is not None:
+            for j, g in zip(top_ids[i], g_top[i]):
+                if 0 <= j < v:
+                    out[i] += g * of_word(int(j))
+    return scale * out

@@ -130,6 +130,15 @@ class burst_cache_t(C.Structure):
                 ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
+class burst_tree_t(C.Structure):
+    _fields_ = [("seen", C.c_void_p), ("seen_stride", C.c_int64), ("first_row", C.c_void_p), ("first_stride", C.c_int64),
+                ("tokens", C.c_void_p), ("sink_rows", C.c_int32), ("elsewhere", C.c_int32)]
+
+
+class burst_scores_shape_t(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64), ("vocab", C.c_int64), ("n_top", C.c_int32), ("scale", C.c_float)]
+
+
 _lib.burst_attn_rope.restype = C.c_int
 # (tensors of these calls go in as the bytes of their description)
 _lib.burst_attn_rope.argtypes = [_P(burst_shape_t), _P(burst_rope_t)] + [C.c_char_p] * 4 + [C.c_int32, C.c_void_p]
@@ -143,6 +152,27 @@ _lib.burst_attn_decode_plan.argtypes = [_P(burst_shape_t), _P(burst_cache_t), _P
 _lib.burst_attn_decode.restype = C.c_int
 _lib.burst_attn_decode.argtypes = [_P(burst_shape_t), _P(burst_cache_t), C.c_char_p, C.c_void_p, C.c_char_p,
                                    C.c_char_p, C.c_void_p, C.c_int64, C.c_void_p]
+_lib.burst_attn_tree_workspace_bytes.restype = C.c_int64
+_lib.burst_attn_tree_workspace_bytes.argtypes = [_P(burst_shape_t)]
+_lib.burst_attn_tree_plan.restype = C.c_int
+_lib.burst_attn_tree_plan.argtypes = [_P(burst_shape_t), _P(C.c_int32)]
+_lib.burst_attn_tree.restype = C.c_int
+_lib.burst_attn_tree.argtypes = [_P(burst_shape_t), _P(burst_cache_t), _P(burst_tree_t), C.c_char_p, C.c_char_p, C.c_char_p, C.c_void_p,
+                                 C.c_int64, C.c_void_p]
+_lib.burst_attn_cache_copy_pages.restype = C.c_int
+_lib.burst_attn_cache_copy_pages.argtypes = [_P(burst_shape_t), C.c_int32, _P(burst_cache_t), C.c_void_p, C.c_int64, C.c_void_p]
+_lib.burst_attn_cache_keep_rows.restype = C.c_int
+_lib.burst_attn_cache_keep_rows.argtypes = [_P(burst_shape_t), C.c_int32, _P(burst_cache_t), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                            C.c_void_p]
+_lib.burst_lm_head_scores_workspace_bytes.restype = C.c_int64
+_lib.burst_lm_head_scores_workspace_bytes.argtypes = [_P(burst_scores_shape_t)]
+_lib.burst_lm_head_scores_plan.restype = C.c_int
+_lib.burst_lm_head_scores_plan.argtypes = [_P(burst_scores_shape_t), _P(C.c_int32)]
+_lib.burst_lm_head_scores.restype = C.c_int
+_lib.burst_lm_head_scores.argtypes = [_P(burst_scores_shape_t), C.c_void_p, C.c_int32, C.c_int64] + [C.c_void_p] * 7 + [C.c_int64, C.c_void_p]
+_lib.burst_lm_head_scores_bwd.restype = C.c_int
+_lib.burst_lm_head_scores_bwd.argtypes = [_P(burst_scores_shape_t), C.c_void_p, C.c_int32, C.c_int64] + [C.c_void_p] * 9 + [C.c_int32, C.c_int64,
+                                                                                                                      C.c_void_p]
 _lib.burst_attn_status_string.restype = C.c_char_p
 _lib.burst_attn_status_string.argtypes = [C.c_int]
 _lib.burst_attn_last_hip_error.restype = C.c_int
@@ -155,7 +185,9 @@ EXPORTS = ["burst_attn_step_fwd", "burst_attn_steps_fwd", "burst_attn_steps_bwd"
            "burst_attn_visible_pairs", "burst_attn_tile_class", "burst_attn_visible_tile_runs", "burst_attn_visible_rows", "burst_attn_mfma_probe", "burst_attn_set_chunk_rows", "burst_attn_chunk_plan", "burst_attn_launch_plan", "burst_attn_status_string", "burst_attn_last_hip_error",
            "burst_attn_version", "burst_lm_head_workspace_bytes", "burst_lm_head_loss",
            "burst_lm_head_static_scratch_bytes", "burst_lm_head_tile_plan", "burst_lm_head_loss_noalloc",
-           "burst_attn_rope", "burst_attn_cache_append", "burst_attn_decode_workspace_bytes", "burst_attn_decode", "burst_attn_decode_plan"]
+           "burst_attn_rope", "burst_attn_cache_append", "burst_attn_decode_workspace_bytes", "burst_attn_decode", "burst_attn_decode_plan",
+           "burst_attn_tree_workspace_bytes", "burst_attn_tree", "burst_attn_tree_plan", "burst_attn_cache_copy_pages", "burst_attn_cache_keep_rows",
+           "burst_lm_head_scores_workspace_bytes", "burst_lm_head_scores", "burst_lm_head_scores_bwd", "burst_lm_head_scores_plan"]
 
 
 class BurstError(RuntimeError):
@@ -606,6 +638,177 @@ def burst_attn_decode_plan(shp, cache):
     out = (C.c_int32 * 3)()
     _check(_lib.burst_attn_decode_plan(shp, cache, out))
     return out[0], out[1], bool(out[2])
+
+
+def tree(seen=None, first_row=None, tokens=None, sink_rows=0, elsewhere=False):
+    """What new tokens see: seen int64 [batch, sq] (the bits of a word for each token; None: a chain), first_row int32 [batch, sq] (of the older rows),
+    tokens int32 [batch] (how many a sequence brings; None: sq), the first sink_rows rows always, elsewhere: their own rows are in another cache.
+    A plan that a program keeps; it holds the tensors, whose contents are read when a call that uses it runs."""
+    device = torch.cuda.current_device()
+    _check_device(device, seen, first_row, tokens)
+    t = burst_tree_t(None, 0, None, 0, None, sink_rows, int(elsewhere))
+    sizes = [None, None]                # batch, sq: of the tensors that there are
+    for name, x, dtype in (("seen", seen, torch.int64), ("first_row", first_row, torch.int32), ("tokens", tokens, torch.int32)):
+        if x is None:
+            continue
+        dims = 1 if name == "tokens" else 2
+        if x.dtype != dtype or x.dim() != dims or (x.size(-1) > 1 and x.stride(-1) != 1):
+            raise ValueError(f"{name}: {dtype} tensor of {dims} dimensions with a contiguous last one expected")
+        for i, n in enumerate(x.shape):
+            if sizes[i] not in (None, n):
+                raise ValueError("seen and first_row [batch, sq], tokens [batch] expected")
+            sizes[i] = n
+        setattr(t, name, x.data_ptr())
+        if dims == 2:
+            setattr(t, "seen_stride" if name == "seen" else "first_stride", x.stride(0) if x.size(0) > 1 else 0)
+    t._tensors, t._sizes, t._device = (seen, first_row, tokens), tuple(sizes), device
+    return t
+
+
+def burst_attn_tree_workspace_bytes(shp):
+    n = _lib.burst_attn_tree_workspace_bytes(C.byref(shp))
+    if n < 0:
+        raise BurstError(BURST_ERR_INVALID_ARG)
+    return n
+
+
+def burst_attn_tree(shp, cache, tree, q, o, lse=None, workspace=None, stream=None):
+    """q [batch, sq, q_heads, head_dim] bf16, new tokens of every sequence, over the cache's rows that the tree says: o (bf16 or fp32), lse [batch,
+    q_heads, sq].  shp.sk bounds the rows of a sequence; workspace: a one-byte tensor of burst_attn_tree_workspace_bytes(shp) bytes."""
+    stream, device = _current(stream)
+    batch, sq, q_heads, kv_heads, d = shp.batch, shp.sq, shp.q_heads, shp.kv_heads, shp.head_dim
+    _check_cache(cache, batch, kv_heads, d, device)
+    if tree._device != device:
+        raise _elsewhere(tree, device)
+    if tree._sizes[0] not in (None, batch) or tree._sizes[1] not in (None, sq):
+        raise ValueError(f"the tree is of {tree._sizes}, not of {(batch, sq)} sequences and tokens")
+    sizes, ws, n = (batch, sq, q_heads, d), None, 0
+    if lse is not None:
+        stride = lse.stride()
+        if lse.shape != (batch, q_heads, sq) or lse.dtype != torch.float32 or (sq > 1 and stride[2] != 1):
+            raise ValueError(f"lse: fp32 tensor of {(batch, q_heads, sq)} with a contiguous last dimension expected")
+        if lse.get_device() != device:
+            _check_device(device, lse)
+        lse = _pack_rowvec(lse.data_ptr(), stride[0], stride[1])
+    if workspace is not None:
+        if workspace.get_device() != device:
+            _check_device(device, workspace)
+        ws, n = workspace.data_ptr(), workspace.nbytes
+    _check(_lib.burst_attn_tree(shp, cache, tree, _packed(q, device, sizes), _packed(o, device, sizes), lse, ws, n, stream))
+
+
+def burst_attn_tree_plan(shp):
+    """(shares, columns of a work-group, whether nothing is dealt) of a burst_attn_tree (diagnostics)."""
+    out = (C.c_int32 * 3)()
+    _check(_lib.burst_attn_tree_plan(shp, out))
+    return out[0], out[1], bool(out[2])
+
+
+def cache_layers(caches):
+    """Caches of a model's layers (paged_cache), for calls that move pages or rows in all of them.  A handle that a program keeps; it holds them."""
+    caches = list(caches)
+    if not caches or any(c._device != caches[0]._device or c._sizes != caches[0]._sizes for c in caches):
+        raise ValueError("caches of one device, batch, kv_heads and head_dim expected")
+    layers = (burst_cache_t * len(caches))(*caches)
+    layers._caches, layers._device = caches, caches[0]._device
+    batch, kv_heads, d = caches[0]._sizes
+    layers._shape = burst_shape_t(batch, kv_heads, kv_heads, d, 0, 0, 1.0)
+    return layers
+
+
+def burst_attn_cache_copy_pages(layers, moves, stream=None):
+    """moves int32 [n, 3]: from, to, rows: the first rows of a page to another page, in all layers."""
+    stream, device = _current(stream)
+    if layers._device != device:
+        raise _elsewhere(layers, device)
+    if moves.get_device() != device:
+        _check_device(device, moves)
+    if moves.dtype != torch.int32 or moves.dim() != 2 or moves.size(1) != 3 or not moves.is_contiguous():
+        raise ValueError("moves: contiguous int32 tensor of [n, 3] expected")
+    _check(_lib.burst_attn_cache_copy_pages(layers._shape, len(layers), layers, moves.data_ptr(), moves.size(0), stream))
+
+
+def burst_attn_cache_keep_rows(layers, from_rows, kept, new_rows=None, stream=None):
+    """from_rows int32 [batch, sq]: of a sequence's last new_rows[b] rows (sq) row from_rows[b][i] becomes row i, for i < kept[b], in all layers."""
+    stream, device = _current(stream)
+    if layers._device != device:
+        raise _elsewhere(layers, device)
+    if from_rows.get_device() != device:
+        _check_device(device, from_rows)
+    s = layers._shape
+    if from_rows.dim() != 2 or from_rows.size(0) != s.batch:
+        raise ValueError(f"from_rows: int32 tensor of [{s.batch}, sq] expected")
+    ptr, kept_ptr, new = _int32(from_rows, 2), _numbers(kept, device, s.batch), _numbers(new_rows, device, s.batch)
+    shp = burst_shape_t(s.batch, s.q_heads, s.kv_heads, s.head_dim, from_rows.size(1), 0, 1.0)
+    _check(_lib.burst_attn_cache_keep_rows(shp, len(layers), layers, ptr, from_rows.stride(0) if s.batch > 1 else 0, new, kept_ptr, stream))
+
+
+def scores_shape(n_tokens, vocab, n_top=0, scale=1.0):
+    return burst_scores_shape_t(n_tokens, vocab, n_top, scale)
+
+
+def burst_lm_head_scores_workspace_bytes(shp):
+    n = _lib.burst_lm_head_scores_workspace_bytes(C.byref(shp))
+    if n < 0:
+        raise BurstError(BURST_ERR_INVALID_ARG)
+    return n
+
+
+def burst_lm_head_scores_plan(shp):
+    """(waves that take a part of a row together, parts of a row) of a burst_lm_head_scores (diagnostics)."""
+    out = (C.c_int32 * 2)()
+    _check(_lib.burst_lm_head_scores_plan(shp, out))
+    return out[0], out[1]
+
+
+def _logits(t, shp, device, name):
+    """Address, type and row stride of a matrix of logits or of their gradient."""
+    n, v = shp.n_tokens, shp.vocab
+    if t.shape != (n, v) or (v > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: tensor of {(n, v)} with a contiguous last dimension expected, not {tuple(t.shape)}, strides {t.stride()}")
+    if t.get_device() != device:
+        _check_device(device, t)
+    return t.data_ptr(), _DTYPES[t.dtype], t.stride(0) if n > 1 else v
+
+
+def _per_token(t, dtype, sizes, device):
+    """The address of a contiguous tensor of these sizes, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != sizes or not t.is_contiguous():
+        raise ValueError(f"contiguous {dtype} tensor of {sizes} expected, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    if t.get_device() != device:
+        _check_device(device, t)
+    return t.data_ptr()
+
+
+def burst_lm_head_scores(shp, logits, y=None, logp=None, lse=None, entropy=None, top_logp=None, top_ids=None, workspace=None, stream=None):
+    """logits [n, vocab] bf16 or fp32 (rows may be strided), y int64 [n]: logp, lse, entropy fp32 [n], top_logp fp32 and top_ids int64 [n, n_top];
+    workspace: a one-byte tensor of burst_lm_head_scores_workspace_bytes(shp) bytes."""
+    stream, device = _current(stream)
+    n, ws, ws_bytes = (shp.n_tokens,), None, 0
+    top = (shp.n_tokens, shp.n_top)
+    if workspace is not None:
+        if workspace.get_device() != device:
+            _check_device(device, workspace)
+        ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
+    f32, i64 = torch.float32, torch.int64
+    _check(_lib.burst_lm_head_scores(shp, *_logits(logits, shp, device, "logits"), _per_token(y, i64, n, device), _per_token(logp, f32, n, device),
+                                     _per_token(lse, f32, n, device), _per_token(entropy, f32, n, device), _per_token(top_logp, f32, top, device),
+                                     _per_token(top_ids, i64, top, device), ws, ws_bytes, stream))
+
+
+def burst_lm_head_scores_bwd(shp, logits, lse, d_logits, y=None, entropy=None, top_ids=None, g_logp=None, g_lse=None, g_entropy=None, g_top=None,
+                             stream=None):
+    """The gradient of the logits, d_logits [n, vocab] bf16 or fp32 (logits itself, too), from those of the scores: g_logp, g_lse, g_entropy fp32
+    [n], g_top fp32 [n, n_top]."""
+    stream, device = _current(stream)
+    n, top = (shp.n_tokens,), (shp.n_tokens, shp.n_top)
+    f32, i64 = torch.float32, torch.int64
+    _check(_lib.burst_lm_head_scores_bwd(shp, *_logits(logits, shp, device, "logits"), _per_token(y, i64, n, device), _per_token(lse, f32, n, device),
+                                         _per_token(entropy, f32, n, device), _per_token(top_ids, i64, top, device),
+                                         _per_token(g_logp, f32, n, device), _per_token(g_lse, f32, n, device), _per_token(g_entropy, f32, n, device),
+                                         _per_token(g_top, f32, top, device), *_logits(d_logits, shp, device, "d_logits"), stream))
 
 
 def burst_attn_mfma_probe(random_operands, iterations, stream=None):

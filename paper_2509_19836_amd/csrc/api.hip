@@ -676,6 +676,162 @@ int burst_attn_decode_plan(const burst_shape_t* shape, const burst_cache_t* cach
   return BURST_OK;
 }
 
+static int check_tree_shape(const burst_shape_t* shape) {
+  BURST_TRY(check_shape(shape));
+  if (shape->sq < 1) return BURST_ERR_INVALID_ARG;
+  // new tokens are bits of a word; launches of less than 2^32 threads; 32-bit numbers of units of 64 rows
+  if (shape->sq > BURST_TREE_MAX_TOKENS || (int64_t)shape->batch * shape->q_heads > (1 << 25) / shape->sq || shape->batch * (shape->sk / 32 + 2) > INT32_MAX)
+    return BURST_ERR_UNSUPPORTED;
+  return BURST_OK;
+}
+
+static int64_t tree_bytes(const burst_shape_t* s) {
+  return tree_workspace_bytes(s->batch, (int32_t)s->sq, s->q_heads, s->kv_heads, s->head_dim, s->sk);
+}
+
+int64_t burst_attn_tree_workspace_bytes(const burst_shape_t* shape) { return check_tree_shape(shape) == BURST_OK ? tree_bytes(shape) : -1; }
+
+int burst_attn_tree(const burst_shape_t* shape, const burst_cache_t* cache, const burst_tree_t* tree, const burst_tensor_t* q, const burst_tensor_t* o,
+                    const burst_rowvec_t* lse, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  BURST_TRY(check_tree_shape(shape));
+  TreeParams p;
+  std::memset(&p, 0, sizeof(p));
+  BURST_TRY(check_cache(cache, shape, &p.cache));
+  if (shape->sk > (int64_t)p.cache.table_cols * p.cache.page_rows) return BURST_ERR_INVALID_ARG;
+  if (!tree || tree->sink_rows < 0) return BURST_ERR_INVALID_ARG;
+  if ((tree->seen && ((uintptr_t)tree->seen & 7)) || (tree->first_row && !aligned4(tree->first_row)) || (tree->tokens && !aligned4(tree->tokens)))
+    return BURST_ERR_INVALID_ARG;
+  for (int64_t stride : {tree->seen ? tree->seen_stride : 0, tree->first_row ? tree->first_stride : 0})
+    if (stride != 0 && (stride < shape->sq || stride > ((int64_t)1 << 58) / shape->batch)) return BURST_ERR_INVALID_ARG;
+  BURST_TRY(check_tensor(q, 1, &p.q));
+  BURST_TRY(check_tensor(o, 3, &p.o));
+  BURST_TRY(check_no_overlap(p.o, shape->batch, shape->sq, shape->q_heads, shape->head_dim));
+  if (lse) {
+    BURST_TRY(check_rowvec(lse, &p.lse));
+    BURST_TRY(check_rowvec_no_overlap(p.lse, shape->batch, shape->q_heads, shape->sq));
+  }
+  const int64_t need = tree_bytes(shape);
+  if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return BURST_ERR_INVALID_ARG;
+  p.batch = shape->batch;
+  p.sq = (int32_t)shape->sq;
+  p.q_heads = shape->q_heads;
+  p.kv_heads = shape->kv_heads;
+  p.head_dim = shape->head_dim;
+  p.max_rows = (int32_t)shape->sk;
+  p.scale = shape->scale;
+  p.seen = tree->seen;
+  p.seen_sb = tree->seen_stride;
+  p.first = tree->first_row;
+  p.first_sb = tree->first_stride;
+  p.tokens = tree->tokens;
+  p.sinks = tree->sink_rows;
+  p.elsewhere = tree->elsewhere != 0;
+  p.workspace = workspace;
+  const hipError_t e = launch_tree(p, (hipStream_t)hip_stream);
+  return e == hipSuccess ? BURST_OK : hip_fail(e);
+}
+
+int burst_attn_tree_plan(const burst_shape_t* shape, int32_t out[3]) {
+  BURST_TRY(check_tree_shape(shape));
+  if (!out) return BURST_ERR_INVALID_ARG;
+  TreeParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.batch = shape->batch;
+  p.sq = (int32_t)shape->sq;
+  p.q_heads = shape->q_heads;
+  p.kv_heads = shape->kv_heads;
+  p.head_dim = shape->head_dim;
+  p.max_rows = (int32_t)shape->sk;
+  tree_plan(p, out);
+  return BURST_OK;
+}
+
+// The keys and values of layers that are written, alike but for where they lie; no two of them, nor a layer's keys and values, at one place.  at: the
+// first layer of those that a launch takes.
+static int check_layers(const burst_shape_t* shape, int32_t n_layers, const burst_cache_t* caches, bool one_table, CacheDev* first) {
+  BURST_TRY(check_shape(shape));
+  if (n_layers < 1 || !caches) return BURST_ERR_INVALID_ARG;
+  if (n_layers > BURST_CACHE_MAX_LAYERS) return BURST_ERR_UNSUPPORTED;
+  const void* places[2 * BURST_CACHE_MAX_LAYERS];
+  for (int32_t i = 0; i < n_layers; ++i) {
+    CacheDev c;
+    BURST_TRY(check_cache(caches + i, shape, &c));
+    if (i == 0) *first = c;
+    if (c.is_f8 != first->is_f8 || c.s_page != first->s_page || c.s_row != first->s_row || c.s_head != first->s_head || c.n_pages != first->n_pages ||
+        c.page_rows != first->page_rows)
+      return BURST_ERR_INVALID_ARG;
+    if (one_table && (c.table != first->table || c.table_stride != first->table_stride || c.table_cols != first->table_cols || c.rows != first->rows))
+      return BURST_ERR_INVALID_ARG;
+    places[2 * i] = c.k;
+    places[2 * i + 1] = c.v;
+  }
+  std::sort(places, places + 2 * n_layers);
+  if (std::adjacent_find(places, places + 2 * n_layers) != places + 2 * n_layers) return BURST_ERR_INVALID_ARG;
+  const TensorDev pages{first->k, first->s_page, first->s_row, first->s_head, 0};
+  BURST_TRY(check_no_overlap(pages, first->n_pages, first->page_rows, shape->kv_heads, shape->head_dim));
+  if ((int64_t)first->page_rows * shape->kv_heads * shape->head_dim > INT32_MAX) return BURST_ERR_UNSUPPORTED;   // 32-bit numbers of a page's elements
+  return BURST_OK;
+}
+
+static void fill_layers(const burst_shape_t* shape, const burst_cache_t* caches, int32_t n, const CacheDev& c, LayersDev* out) {
+  std::memset(out, 0, sizeof(*out));
+  for (int32_t i = 0; i < n; ++i) {
+    out->k[i] = caches[i].k.ptr;
+    out->v[i] = caches[i].v.ptr;
+  }
+  out->n = n;
+  out->kv_heads = shape->kv_heads;
+  out->head_dim = shape->head_dim;
+  out->page_rows = c.page_rows;
+  out->n_pages = c.n_pages;
+  out->bytes = c.is_f8 ? 1 : 2;
+  out->head_outer = c.s_head > c.s_row;
+  out->s_page = c.s_page * out->bytes;
+  out->s_row = c.s_row * out->bytes;
+  out->s_head = c.s_head * out->bytes;
+}
+
+int burst_attn_cache_copy_pages(const burst_shape_t* shape, int32_t n_layers, const burst_cache_t* caches, const int32_t* moves, int64_t n_moves,
+                                void* hip_stream) {
+  CacheDev c;
+  BURST_TRY(check_layers(shape, n_layers, caches, false, &c));
+  if (n_moves < 0 || (n_moves > 0 && !aligned4(moves))) return BURST_ERR_INVALID_ARG;
+  if (n_moves > INT32_MAX) return BURST_ERR_UNSUPPORTED;
+  for (int32_t i = 0; i < n_layers && n_moves > 0; i += kLayersOfLaunch) {
+    CopyPagesParams p;
+    fill_layers(shape, caches + i, std::min(kLayersOfLaunch, n_layers - i), c, &p.layers);
+    p.moves = moves;
+    p.n_moves = (int32_t)n_moves;
+    const hipError_t e = launch_cache_copy_pages(p, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e);
+  }
+  return BURST_OK;
+}
+
+int burst_attn_cache_keep_rows(const burst_shape_t* shape, int32_t n_layers, const burst_cache_t* caches, const int32_t* from, int64_t from_stride,
+                               const int32_t* new_rows, const int32_t* kept, void* hip_stream) {
+  CacheDev c;
+  BURST_TRY(check_layers(shape, n_layers, caches, true, &c));
+  if (shape->sq > BURST_TREE_MAX_TOKENS) return BURST_ERR_UNSUPPORTED;
+  if (shape->sq == 0) return BURST_OK;
+  if (!aligned4(from) || !aligned4(kept) || (new_rows && !aligned4(new_rows))) return BURST_ERR_INVALID_ARG;
+  if (from_stride != 0 && (from_stride < shape->sq || from_stride > ((int64_t)1 << 60) / shape->batch)) return BURST_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n_layers; i += kLayersOfLaunch) {
+    KeepRowsParams p;
+    fill_layers(shape, caches + i, std::min(kLayersOfLaunch, n_layers - i), c, &p.cache.layers);
+    p.cache.dev = c;
+    p.batch = shape->batch;
+    p.sq = (int32_t)shape->sq;
+    p.from = from;
+    p.from_sb = from_stride;
+    p.new_rows = new_rows;
+    p.kept = kept;
+    const hipError_t e = launch_cache_keep_rows(p, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e);
+  }
+  return BURST_OK;
+}
+
 static int fill_common(int32_t dev_i, int32_t shard_j, int32_t G, int64_t N, burst_mask_t* out) {
   if (!out || G < 1 || dev_i < 0 || dev_i >= G || shard_j < 0 || shard_j >= G || N < 0) return BURST_ERR_INVALID_ARG;
   std::memset(out, 0, sizeof(*out));
@@ -1009,6 +1165,102 @@ int burst_lm_head_loss(const burst_lm_head_shape_t* shape, const void* h_last, i
     return BURST_ERR_INVALID_ARG;
   return lm_head_loss_on(shape, h_last, ld_h, w_head, ld_w, y, loss, lse, d_h, d_h_dtype, ld_dh, d_w, ld_dw, accumulate_dw,
                          workspace, hip_stream);
+}
+
+static int check_scores_shape(const burst_scores_shape_t* s) {
+  if (!s || s->n_tokens < 0 || s->vocab < 1 || s->n_top < 0 || s->n_top > s->vocab) return BURST_ERR_INVALID_ARG;
+  if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return BURST_ERR_INVALID_ARG;
+  // (a launch of less than 2^32 threads, 64 a token)
+  if (s->n_top > BURST_SCORES_MAX_TOP || s->vocab > (1 << 30) || s->n_tokens > (1 << 25)) return BURST_ERR_UNSUPPORTED;
+  return BURST_OK;
+}
+
+static int check_logits(const void* logits, int32_t dtype, int64_t ld, const burst_scores_shape_t* s) {
+  if (dtype != BURST_BF16 && dtype != BURST_F32) return BURST_ERR_INVALID_ARG;
+  if (ld < s->vocab || ld > ((int64_t)1 << 34)) return BURST_ERR_INVALID_ARG;   // (row offsets far inside 64 bits)
+  return s->n_tokens > 0 && (!logits || ((uintptr_t)logits & 15)) ? BURST_ERR_INVALID_ARG : BURST_OK;
+}
+
+static bool aligned8(const void* ptr) { return ((uintptr_t)ptr & 7) == 0; }
+
+int64_t burst_lm_head_scores_workspace_bytes(const burst_scores_shape_t* shape) {
+  return check_scores_shape(shape) == BURST_OK ? scores_workspace_bytes(shape->n_tokens, (int32_t)shape->vocab, shape->n_top) : -1;
+}
+
+int burst_lm_head_scores_plan(const burst_scores_shape_t* shape, int32_t out[2]) {
+  BURST_TRY(check_scores_shape(shape));
+  if (!out) return BURST_ERR_INVALID_ARG;
+  scores_plan(shape->n_tokens, (int32_t)shape->vocab, out);
+  return BURST_OK;
+}
+
+int burst_lm_head_scores(const burst_scores_shape_t* shape, const void* logits, int32_t logits_dtype, int64_t ld, const int64_t* y, float* logp, float* lse,
+                         float* entropy, float* top_logp, int64_t* top_ids, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  BURST_TRY(check_scores_shape(shape));
+  BURST_TRY(check_logits(logits, logits_dtype, ld, shape));
+  if (shape->n_tokens == 0) return BURST_OK;
+  if ((y == nullptr) != (logp == nullptr) || !aligned8(y)) return BURST_ERR_INVALID_ARG;
+  for (const float* out : {logp, lse, entropy, top_logp})
+    if (out && !aligned4(out)) return BURST_ERR_INVALID_ARG;
+  if (!aligned8(top_ids) || (shape->n_top == 0 && (top_logp || top_ids))) return BURST_ERR_INVALID_ARG;
+  if (!logp && !lse && !entropy && !top_logp && !top_ids) return BURST_ERR_INVALID_ARG;
+  const int64_t need = scores_workspace_bytes(shape->n_tokens, (int32_t)shape->vocab, shape->n_top);
+  if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return BURST_ERR_INVALID_ARG;
+  ScoresParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.n_tokens = shape->n_tokens;
+  p.ld = ld;
+  p.vocab = (int32_t)shape->vocab;
+  p.n_top = top_logp || top_ids ? shape->n_top : 0;
+  p.scale = shape->scale;
+  p.is_f32 = logits_dtype == BURST_F32;
+  p.logits = logits;
+  p.y = y;
+  p.logp = logp;
+  p.lse = lse;
+  p.entropy = entropy;
+  p.top_logp = top_logp;
+  p.top_ids = top_ids;
+  p.workspace = workspace;
+  const hipError_t e = launch_scores(p, (hipStream_t)hip_stream);
+  return e == hipSuccess ? BURST_OK : hip_fail(e);
+}
+
+int burst_lm_head_scores_bwd(const burst_scores_shape_t* shape, const void* logits, int32_t logits_dtype, int64_t ld, const int64_t* y, const float* lse,
+                             const float* entropy, const int64_t* top_ids, const float* g_logp, const float* g_lse, const float* g_entropy, const float* g_top,
+                             void* d_logits, int32_t d_logits_dtype, int64_t ld_d, void* hip_stream) {
+  BURST_TRY(check_scores_shape(shape));
+  BURST_TRY(check_logits(logits, logits_dtype, ld, shape));
+  BURST_TRY(check_logits(d_logits, d_logits_dtype, ld_d, shape));
+  if (shape->n_tokens == 0) return BURST_OK;
+  if (logits == d_logits && (logits_dtype != d_logits_dtype || ld != ld_d)) return BURST_ERR_INVALID_ARG;
+  if (!g_logp && !g_lse && !g_entropy && !g_top) return BURST_ERR_INVALID_ARG;
+  if (!aligned4(lse) || (g_logp && !y) || (g_entropy && !entropy) || (g_top && (!top_ids || shape->n_top == 0))) return BURST_ERR_INVALID_ARG;
+  for (const float* in : {entropy, g_logp, g_lse, g_entropy, g_top})
+    if (in && !aligned4(in)) return BURST_ERR_INVALID_ARG;
+  if (!aligned8(y) || !aligned8(top_ids)) return BURST_ERR_INVALID_ARG;
+  ScoresBwdParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.n_tokens = shape->n_tokens;
+  p.ld = ld;
+  p.ld_out = ld_d;
+  p.vocab = (int32_t)shape->vocab;
+  p.n_top = shape->n_top;
+  p.scale = shape->scale;
+  p.is_f32 = logits_dtype == BURST_F32;
+  p.out_is_f32 = d_logits_dtype == BURST_F32;
+  p.logits = logits;
+  p.d_logits = d_logits;
+  p.y = y;
+  p.top_ids = top_ids;
+  p.lse = lse;
+  p.entropy = entropy;
+  p.g_logp = g_logp;
+  p.g_lse = g_lse;
+  p.g_entropy = g_entropy;
+  p.g_top = g_top;
+  const hipError_t e = launch_scores_bwd(p, (hipStream_t)hip_stream);
+  return e == hipSuccess ? BURST_OK : hip_fail(e);
 }
 
 int64_t burst_lm_head_static_scratch_bytes(void) { return kStaticScratchBytes; }

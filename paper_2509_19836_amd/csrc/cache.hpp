@@ -92,10 +92,58 @@ struct DecodeParams {
   void* workspace;
 };
 
+struct TreeParams {
+  int32_t batch, sq, q_heads, kv_heads, head_dim;
+  int32_t max_rows;
+  float scale;
+  TensorDev q, o;
+  RowvecDev lse;              // ptr == nullptr: not wanted
+  const uint64_t* seen;       // nullptr: a chain
+  int64_t seen_sb;
+  const int32_t* first;       // nullptr: 0
+  int64_t first_sb;
+  const int32_t* tokens;      // nullptr: sq
+  int32_t sinks, elsewhere;
+  CacheDev cache;
+  void* workspace;
+};
+
+// The keys and values of some layers, alike but for where they are.
+constexpr int kLayersOfLaunch = 64;
+struct LayersDev {
+  void* k[kLayersOfLaunch];
+  void* v[kLayersOfLaunch];
+  int32_t n, kv_heads, head_dim, page_rows, n_pages;
+  int32_t bytes;                     // of an element
+  int32_t head_outer;                // heads are further apart than rows
+  int64_t s_page, s_row, s_head;     // bytes
+};
+struct CopyPagesParams {
+  LayersDev layers;
+  const int32_t* moves;   // [n_moves][3]: from, to, rows
+  int32_t n_moves;
+};
+struct KeepRowsParams {
+  struct {
+    LayersDev layers;
+    CacheDev dev;         // (k and v are not read)
+  } cache;
+  int32_t batch, sq;
+  const int32_t* from;
+  int64_t from_sb;
+  const int32_t* new_rows;   // nullptr: sq
+  const int32_t* kept;
+};
+
 hipError_t launch_rope(const RopeParams& p, hipStream_t stream);
 hipError_t launch_cache_append(const AppendParams& p, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams& p, hipStream_t stream);
 void decode_plan(const DecodeParams& p, int32_t out[3]);   // burst_attn_decode_plan
 int64_t decode_workspace_bytes(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t max_rows);
+hipError_t launch_tree(const TreeParams& p, hipStream_t stream);
+void tree_plan(const TreeParams& p, int32_t out[3]);   // burst_attn_tree_plan
+int64_t tree_workspace_bytes(int32_t batch, int32_t sq, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t max_rows);
+hipError_t launch_cache_copy_pages(const CopyPagesParams& p, hipStream_t stream);
+hipError_t launch_cache_keep_rows(const KeepRowsParams& p, hipStream_t stream);
 
 }  // namespace burst

@@ -338,6 +338,34 @@ int64_t lm_head_workspace_bytes(int64_t tile_tokens, int64_t vocab, int64_t d_mo
 void lm_head_tile_plan(const LmHeadParams& p, int32_t out[6]);   // burst_lm_head_tile_plan, from the sizes in p
 hipError_t launch_lm_head_loss(const LmHeadParams& p, hipStream_t stream);
 
+// Scores of tokens from their logits, and the gradient of the logits (the gradients that come in, and entropy and ids, may be nullptr).
+struct ScoresParams {
+  int64_t n_tokens, ld;
+  int32_t vocab, n_top;
+  float scale;
+  int32_t is_f32;
+  const void* logits;   // [n_tokens][ld]
+  const int64_t* y;
+  float *logp, *lse, *entropy;   // may be nullptr
+  float* top_logp;      // [n_tokens][n_top], may be nullptr
+  int64_t* top_ids;
+  void* workspace;
+};
+struct ScoresBwdParams {
+  int64_t n_tokens, ld, ld_out;
+  int32_t vocab, n_top;
+  float scale;
+  int32_t is_f32, out_is_f32;
+  const void* logits;
+  void* d_logits;       // [n_tokens][ld_out]
+  const int64_t *y, *top_ids;
+  const float *lse, *entropy, *g_logp, *g_lse, *g_entropy, *g_top;
+};
+hipError_t launch_scores(const ScoresParams& p, hipStream_t stream);
+hipError_t launch_scores_bwd(const ScoresBwdParams& p, hipStream_t stream);
+int64_t scores_workspace_bytes(int64_t n_tokens, int32_t vocab, int32_t n_top);
+void scores_plan(int64_t n_tokens, int32_t vocab, int32_t out[2]);   // burst_lm_head_scores_plan
+
 // n steps of the query chunk that `p` describes (its own step array is not read).  More than one only without o_part.
 // With a log nothing is launched: it gets the kernel (BURST_KERNEL_ bits) of each launch of step kernels that there would be.
 typedef std::vector<int32_t> LaunchLog;
