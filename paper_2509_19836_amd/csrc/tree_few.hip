@@ -1,0 +1,161 @@
+// Attention of a few new tokens over a paged cache where they are up to 32 columns (new tokens times query heads of a key head): the cache's bytes bound it.
+//
+// Each wave has tiles of 32 rows of its own and all columns: it brings its keys and values to its own part of LDS and meets the others only at the end,
+// so loads stay under way everywhere.
+#include "tree.hpp"
+
+namespace burst {
+
+namespace {
+
+// NW: waves of a work-group, four where rows are dealt to many, eight where a work-group has a whole sequence.
+template <int D, bool F8, bool PAGES16, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void tree_few_kernel(TreeParams, TreeSpace ws, int32_t shares, int32_t direct) {
+  using Columns = TreeColumns<D, F8, 3, D == 128 && !F8 && !PAGES16 ? 1 : 4>;   // (registers)
+  using Run = TreeRun<D, F8, PAGES16, 2>;
+  using Operands = TreeOperands<D, F8>;
+  constexpr int NB = Columns::NB, DB = Columns::DB, UNIT = 32 * NW, TILE = Operands::TILE, NI = Run::NI;
+  constexpr int SLOTS = F8 ? 2 : 1, LOADS = 2 * NI * (2 * SLOTS - 1);   // tiles under way; loads behind those that a product waits for
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [wave][slot][K tile, V tile], maxima and sums [wave][32]
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, g = lane >> 4;
+  char* const tiles = smem + wave * SLOTS * 2 * TILE;
+  const uint32_t tiles0 = (uint32_t)(uintptr_t)(lds_bytes)tiles;
+  float2* const ml_lds = (float2*)(smem + NW * SLOTS * 2 * TILE);
+  const TreeParams& sizes = args_here();
+  const int32_t kv_heads = sizes.kv_heads, group = sizes.q_heads / kv_heads;
+  const int32_t share = (int32_t)((uint32_t)blockIdx.x / (uint32_t)kv_heads), hk = (int32_t)blockIdx.x - share * kv_heads;
+
+  TreeWalk<UNIT> walk;
+  if (!walk.init(args_here(), share, shares, direct != 0, lane)) return;
+  Operands ops;
+  ops.init(lane);
+  do {
+    walk.begin(direct != 0, hk == 0 && tid == 0, ws, share);
+    if (walk.take <= 0) continue;
+    const int32_t b = walk.b, columns = walk.seq.tokens * group;
+    Columns x;
+    x.init(args_here(), walk.seq, b, hk, group, 0, lane);
+    TreeUnion some;
+    some.init(args_here(), walk.seq, b, lane);
+    Run run;
+    run.init(args_here().cache, b, hk, walk.seq.hi, 0, lane);
+
+    // This wave's tiles: rows of unit u from 32 wave on, two runs of 16.  Tile u + SLOTS takes the place of tile u: its keys are asked for when the scores of u
+    // have been formed, its values when the products with P are done.
+    const bool once = direct == 0;   // lines are not kept where rows are many
+    typename Run::Pages pages[2];
+    typename Run::Place place[2];
+    const int32_t end = walk.at + walk.take;
+    uint32_t there[SLOTS];
+    auto first_row = [&](int32_t u) { return walk.row_of(u) + 32 * wave; };
+    auto look_up = [&](int32_t u) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) run.look_up(first_row(u) + 16 * h, lane, pages[h]);
+    };
+    auto put = [&](int32_t u) {
+      const uint32_t rows = (uint32_t)some.rows(first_row(u));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) run.place(first_row(u) + 16 * h, (rows >> (16 * h)) & 0xffffu, lane, pages[h], place[h]);
+      return place[0].there | place[1].there << 16;
+    };
+    auto ask_k = [&](uint32_t kt) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) run.template bring<false>(place[h], h, kt + Run::BYTES * h, once);
+    };
+    auto ask_v = [&](uint32_t vt) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) run.template bring<true>(place[h], h, vt + Run::BYTES * h, once);
+    };
+    look_up(walk.at);
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+      there[i] = 0;
+      if (walk.at + i < end) {
+        there[i] = put(walk.at + i);
+        ask_k(tiles0 + i * 2 * TILE);
+        ask_v(tiles0 + i * 2 * TILE + TILE);
+        if (walk.at + i + 1 < end) look_up(walk.at + i + 1);
+      }
+    }
+    int slot = 0;
+    for (int32_t u = walk.at; u < end; ++u) {
+      const bool more = u + SLOTS < end;
+      const uint32_t kt = tiles0 + slot * 2 * TILE, vt = kt + TILE, now = there[0];
+      if (more) wait_loads<LOADS>();
+      else wait_loads<0>();
+      x.scores(kt, ops);
+#pragma unroll
+      for (int i = 0; i + 1 < SLOTS; ++i) there[i] = there[i + 1];
+      if (more) {
+        there[SLOTS - 1] = put(u + SLOTS);
+        ask_k(kt);
+        if (u + SLOTS + 1 < end) look_up(u + SLOTS + 1);
+      }
+      x.weights(first_row(u), now, g);
+      if (more) wait_loads<LOADS>();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) Run::clear(tiles + (slot * 2 + 1) * TILE + Run::BYTES * h, (now >> (16 * h)) & 0xffffu, lane);
+      x.add(vt, ops);
+      if (more) ask_v(vt);
+      if (SLOTS == 2) slot ^= 1;
+    }
+    x.finish();
+    const TreeParams& p = args_here();
+
+    // The waves' sums against their largest maximum; where their tiles were
+    if (g == 0) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) ml_lds[32 * wave + 16 * nb + r] = float2{x.m[nb], x.l[nb]};
+    }
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem);   // [wave][block of 16 elements][column block][lane]
+    static_assert(DB * NB * 64 * 16 == SLOTS * 2 * TILE, "a wave's sums fit where its tiles were");
+#pragma unroll
+    for (int i = 0; i < DB * NB; ++i) sums[(wave * DB * NB + i) * 64 + lane] = x.acc[i / NB][i % NB];
+    __syncthreads();
+    for (int i = tid; i < DB * NB * 64; i += 64 * NW) {
+      const int at = i / 64, l = i % 64, nb = at % NB, c = 16 * nb + l % 16, d = 16 * (at / NB) + 4 * (l / 16);
+      if (c >= columns) continue;
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) top = fmaxf(top, ml_lds[32 * w + c].x);
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float2 ml = ml_lds[32 * w + c];
+        const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
+        sum += ml.y * f;
+        o += sums[(w * DB * NB + at) * 64 + l] * f;
+      }
+      if (walk.whole) {
+        tree_write<F8>(p, b, hk, group, c, d, o, top, sum);
+      } else {
+        const int64_t piece = (2 * ((int64_t)share * kv_heads + hk) + (walk.first_piece ? 0 : 1)) * 32 + c;
+        *reinterpret_cast<f32x4*>(ws.o + piece * D + d) = o;
+        if (d == 0) ws.ml[piece] = float2{top, sum};
+      }
+    }
+    __syncthreads();
+  } while (walk.next(args_here(), direct != 0));
+}
+
+template <int D, bool F8, bool PAGES16, int NW>
+hipError_t launch(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream) {
+  constexpr int LDS = NW * (32 * 4 * D + 32 * 8);   // (tiles of e4m3 are half as large and twice as many)
+  hipLaunchKernelGGL((tree_few_kernel<D, F8, PAGES16, NW>), dim3((uint32_t)((int64_t)shares * p.kv_heads)), dim3(64 * NW), LDS, stream, p, ws, shares, direct ? 1 : 0);
+  return hipGetLastError();
+}
+template <int D, bool F8>
+hipError_t launch(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream) {
+  const bool pages16 = p.cache.page_rows % 16 == 0;
+  if (direct) return pages16 ? launch<D, F8, true, 8>(p, ws, shares, true, stream) : launch<D, F8, false, 8>(p, ws, shares, true, stream);
+  return pages16 ? launch<D, F8, true, 4>(p, ws, shares, false, stream) : launch<D, F8, false, 4>(p, ws, shares, false, stream);
+}
+
+}  // namespace
+
+hipError_t launch_tree_few(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream) {
+  if (p.head_dim == 128) return p.cache.is_f8 ? launch<128, true>(p, ws, shares, direct, stream) : launch<128, false>(p, ws, shares, direct, stream);
+  return p.cache.is_f8 ? launch<64, true>(p, ws, shares, direct, stream) : launch<64, false>(p, ws, shares, direct, stream);
+}
+
+}  // namespace burst
