@@ -20,19 +20,24 @@ namespace burst {
 namespace {
 
 constexpr int kTreeRows = 64;      // rows of a tile
-constexpr int kTreeWaves = 4;
+constexpr int kTreeWaves = 4;      // of a work-group, two of which share a CU
+constexpr int tree_slots(int head_dim, bool f8) { return (1 << 16) / (2 * kTreeRows * head_dim * (f8 ? 1 : 2)); }   // 64 KiB
 
 // CW: waves side by side, of 32 columns each; the other way they share a tile's rows.
 template <int D, bool F8, bool PAGES16, int CW, int PARTS>
 __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, TreeSpace ws, int32_t blocks, int32_t shares, int32_t direct) {
-  using Columns = TreeColumns<D, F8, PARTS, D == 128 && !F8 && !PAGES16 ? 2 : 4>;   // (registers)
+  constexpr int RW = kTreeWaves / CW, CH = RW == 1 && PARTS == 1 ? 2 : 1, PASSES = 2 / RW / CH;
+  using Columns = TreeColumns<D, F8, 2, PARTS, D == 128 && !F8 && !PAGES16 ? 2 : 4, CH>;   // (registers)
   using Run = TreeRun<D, F8, PAGES16, 1>;
   using Operands = TreeOperands<D, F8>;
-  constexpr int RW = kTreeWaves / CW, HALVES = 2 / RW, NB = Columns::NB, DB = Columns::DB, HALF = Operands::TILE, TILE = 2 * HALF, COLS = 32 * CW;
-  constexpr int SLOTS = F8 ? 4 : 2, LOADS = 2 * Run::NI * (SLOTS - 2);   // tiles in LDS; loads that may be under way when a tile is there
-  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [SLOTS][K tile, V tile], the rows that are there [SLOTS][wave], maxima and sums
+  constexpr int NB = 2, DB = Columns::DB, HALF = Operands::TILE, TILE = 2 * HALF, COLS = 32 * CW;
+  constexpr int SLOTS = tree_slots(D, F8), LOADS = 2 * Run::NI * (SLOTS - 2);   // tiles in LDS; loads that may be under way when one is there
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [SLOTS][K tile, V tile], the rows that are there [SLOTS][4 runs], maxima and sums
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_bytes)smem;
-  volatile uint16_t* const there_lds = (volatile uint16_t*)(smem + SLOTS * 2 * TILE);
+  // (through the address space: a volatile access by a generic pointer is a flat one, which waits for all loads under way)
+  typedef volatile __attribute__((address_space(3))) uint16_t* lds_u16;
+  typedef volatile __attribute__((address_space(3))) uint64_t* lds_u64;
+  const lds_bytes there_lds = (lds_bytes)smem + SLOTS * 2 * TILE;
   float2* const ml_lds = (float2*)(smem + SLOTS * 2 * TILE + SLOTS * 8);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int cw = wave % CW, rw = wave / CW;
@@ -60,7 +65,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
     Run run;
     run.init(args_here().cache, b, hk, walk.seq.hi, wave & 1, lane);
 
-    // A wave brings rows 16 wave .. of a tile, SLOTS - 1 tiles before it is multiplied
+    // A wave brings 16 rows of a tile, SLOTS - 1 tiles before it is multiplied
     const bool once = blocks == 1 && direct == 0;   // lines are not kept where rows are many and no other work-group reads them
     typename Run::Pages pages;
     const int32_t end = walk.at + walk.take;
@@ -73,7 +78,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
       const uint32_t kt = lds0 + slot * 2 * TILE + wave * Run::BYTES;
       run.template bring<false>(place, 0, kt, once);
       run.template bring<true>(place, 0, kt + TILE, once);
-      if (lane == 0) there_lds[slot * kTreeWaves + wave] = (uint16_t)place.there;
+      if (lane == 0) ((lds_u16)there_lds)[slot * 4 + wave] = (uint16_t)place.there;
       return place.there;
     };
     look_up(walk.at);
@@ -95,7 +100,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
       lds_barrier();            // the tile is there, and all waves have left the one before
 #pragma unroll
       for (int i = 0; i + 2 < SLOTS; ++i) there[i] = there[i + 1];
-      const uint64_t rows_there = uniform(*reinterpret_cast<const volatile uint64_t*>(there_lds + slot * kTreeWaves));
+      const uint64_t rows_there = uniform(((lds_u64)there_lds)[slot]);
       if (u + SLOTS - 1 < end) {
         there[SLOTS - 2] = ask(u + SLOTS - 1, next_slot);
         if (u + SLOTS < end) look_up(u + SLOTS);
@@ -104,10 +109,10 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
         const uint32_t kt = lds0 + slot * 2 * TILE;
         const int32_t t0 = walk.row_of(u);
 #pragma clang loop unroll(disable)
-        for (int i = 0; i < HALVES; ++i) {   // (the scores and P of 64 rows do not fit in the registers beside the sums)
+        for (int i = 0; i < PASSES; ++i) {   // (with P in three parts the scores and P of 64 rows do not fit in the registers beside the sums)
           const int half = RW == 2 ? rw : i;
           x.scores(kt + half * HALF, ops);
-          x.weights(t0 + 32 * half, (uint32_t)(rows_there >> (32 * half)), g);
+          x.weights(t0 + 32 * half, rows_there >> (32 * half) & low_bits(32 * CH), g);
           x.add(kt + TILE + half * HALF, ops);
         }
       }
@@ -162,43 +167,74 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
   } while (walk.next(args_here(), direct != 0));
 }
 
-// A (sequence, new token, query head) whose rows several work-groups had: their pieces added up.  D / 4 threads for each.
-template <int D, int COLS>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeParams p, TreeSpace ws, int32_t blocks) {
-  constexpr int LANES = D / 4;
-  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
-  const int lane = threadIdx.x % LANES;
-  const int32_t h = (int32_t)(row % p.q_heads), group = p.q_heads / p.kv_heads, hk = h / group;
-  const int64_t bi = row / p.q_heads;
-  const int32_t b = (int32_t)(bi / p.sq), i = (int32_t)(bi - (int64_t)b * p.sq);
+// A (sequence, new token, query head) whose rows several work-groups had: their pieces added up, in a fixed order.  GROUPS times D / 4 threads take every
+// GROUPS-th piece each, four at a time against a running maximum; with GROUPS > 1 their sums meet in LDS.
+template <int D, int COLS, int GROUPS>
+__global__ __launch_bounds__(GROUPS == 1 ? 256 : GROUPS * D / 4) void tree_join_kernel(TreeParams p, TreeSpace ws, int32_t blocks) {
+  constexpr int LANES = D / 4, U = 4, OUTPUTS = GROUPS == 1 ? 256 / LANES : 1;
+  __shared__ f32x4 part[GROUPS == 1 ? 1 : GROUPS][LANES];
+  __shared__ float2 part_ml[GROUPS];
+  const int lane = threadIdx.x % LANES, group_of = GROUPS == 1 ? 0 : threadIdx.x / LANES;
+  const uint32_t row = blockIdx.x * OUTPUTS + (GROUPS == 1 ? threadIdx.x / LANES : 0);   // (below 2^25, checked on the host)
+  const int32_t bi = (int32_t)(row / (uint32_t)p.q_heads), h = (int32_t)row - bi * p.q_heads, group = p.q_heads / p.kv_heads, hk = h / group;
+  const int32_t b = bi / p.sq, i = bi - b * p.sq;
   if (b >= p.batch) return;
-  int32_t tokens = p.tokens ? p.tokens[b] : p.sq;
+  const int32_t tokens = p.tokens ? p.tokens[b] : p.sq;
+  const int2 owners = ws.owners[b];   // (not written for a sequence without tokens)
   if (i >= tokens) return;
-  const int2 owners = ws.owners[b];
   const int32_t w0 = owners.x, w1 = owners.y >> 1, skip = owners.y & 1;
   if (w0 == w1) return;   // written out by its only owner
   const int32_t c = i * group + (h - hk * group), hb = hk * blocks + c / COLS, per_seq = p.kv_heads * blocks;
   auto piece = [&](int32_t w) { return (2 * ((int64_t)w * per_seq + hb) + (w == w0 ? skip : 0)) * COLS + c % COLS; };
   float top = -INFINITY, sum = 0.f;
-  for (int32_t w = w0; w <= w1; ++w) top = fmaxf(top, ws.ml[piece(w)].x);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int32_t w = w0; w <= w1; ++w) {
-    const int64_t at = piece(w);
-    const float2 ml = ws.ml[at];
-    const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
-    sum += ml.y * f;
-    o += *reinterpret_cast<const f32x4*>(ws.o + at * D + 4 * lane) * f;
+  for (int32_t w = w0 + group_of; w <= w1; w += U * GROUPS) {
+    float2 ml[U];
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = piece(min(w + u * GROUPS, w1));
+      ml[u] = ws.ml[at];
+      x[u] = *reinterpret_cast<const f32x4*>(ws.o + at * D + 4 * lane);
+    }
+    float up = top;
+#pragma unroll
+    for (int u = 0; u < U; ++u) up = fmaxf(up, w + u * GROUPS <= w1 ? ml[u].x : -INFINITY);
+    const float f0 = top == up ? 1.f : __builtin_amdgcn_exp2f(top - up);
+    top = up;
+    sum *= f0;
+    o *= f0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (w + u * GROUPS > w1) continue;
+      const float f = ml[u].x == top ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - top);
+      sum += ml[u].y * f;
+      o += x[u] * f;
+    }
   }
-  o *= sum == 0.f ? 0.f : (p.cache.v_scale ? p.cache.v_scale[hk] : 1.f) / sum;
-  const int64_t to = b * p.o.sb + i * p.o.ss + h * p.o.sh + 4 * lane;
-  if (p.o.is_f32) *reinterpret_cast<f32x4*>((float*)p.o.ptr + to) = o;
-  else *reinterpret_cast<bf16x4*>((__bf16*)p.o.ptr + to) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
-  if (lane == 0 && p.lse.ptr) p.lse.ptr[b * p.lse.sb + h * p.lse.sh + i] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
+  if constexpr (GROUPS > 1) {
+    part[group_of][lane] = o;
+    if (lane == 0) part_ml[group_of] = float2{top, sum};
+    __syncthreads();
+    if (group_of != 0) return;
+    top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, part_ml[k].x);
+    sum = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int k = 0; k < GROUPS; ++k) {
+      const float f = part_ml[k].x == top ? 1.f : __builtin_amdgcn_exp2f(part_ml[k].x - top);
+      sum += part_ml[k].y * f;
+      o += part[k][lane] * f;
+    }
+  }
+  if (p.cache.is_f8) tree_write<true>(p, b, hk, group, c, 4 * lane, o, top, sum);
+  else tree_write<false>(p, b, hk, group, c, 4 * lane, o, top, sum);
 }
 
 // How a call is dealt.
-constexpr int kTreeFit = 512;      // work-groups of four waves that the chip holds at once, two a CU
+constexpr int kTreeFit = 512;      // work-groups that the chip holds at once, two a CU
 struct TreeShape {
   int32_t columns, blocks, shares;   // columns of a work-group; blocks of them of a key head; shares of the units
   bool direct;                       // a share for every sequence, no workspace
@@ -208,10 +244,10 @@ int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 TreeShape tree_shape(int32_t batch, int32_t sq, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t max_rows) {
   TreeShape s;
   const int32_t all = q_heads / kv_heads * sq;
-  s.columns = all <= 32 ? 32 : all <= 64 ? 64 : 128;
+  s.columns = all <= 16 ? 16 : all <= 32 ? 32 : all <= 64 ? 64 : 128;
   s.blocks = (all + s.columns - 1) / s.columns;
-  const int64_t per_seq = (int64_t)kv_heads * s.blocks, unit = s.columns == 32 ? 128 : 64, max_units = std::max<int64_t>(1, (max_rows + unit - 1) / unit);
-  s.direct = batch * per_seq >= kTreeFit || max_rows * head_dim <= (s.columns == 32 ? 512 * 128 : 128 * 128);
+  const int64_t per_seq = (int64_t)kv_heads * s.blocks, unit = s.columns <= 32 ? 128 : 64, max_units = std::max<int64_t>(1, (max_rows + unit - 1) / unit);
+  s.direct = batch * per_seq >= kTreeFit || max_rows * head_dim <= (s.columns <= 32 ? 512 * 128 : 128 * 128);
   s.shares = (int32_t)(s.direct ? batch : std::min<int64_t>(batch * max_units, std::max<int64_t>(1, kTreeFit / per_seq)));
   const int64_t pieces = s.shares * per_seq * 2 * s.columns;
   s.off_ml = up256((int64_t)batch * 8);
@@ -223,7 +259,8 @@ TreeShape shape_of(const TreeParams& p) { return tree_shape(p.batch, p.sq, p.q_h
 
 template <int D, bool F8, bool PAGES16, int CW, int PARTS>
 hipError_t launch_columns(const TreeParams& p, const TreeShape& s, const TreeSpace& ws, hipStream_t stream) {
-  constexpr int LDS = 2 * 2 * kTreeRows * 2 * D + 4 * 8 + 64 * 8;   // (tiles of e4m3 are half as large and twice as many)
+  constexpr int SLOTS = tree_slots(D, F8), LDS = SLOTS * (2 * kTreeRows * D * (F8 ? 1 : 2) + 8) + 64 * 8;
+  static_assert(LDS >= 2 * 32 * D * 4 + 64 * 8, "sums of two waves fit where the tiles were");
   const int64_t pairs = ((int64_t)s.shares * p.kv_heads + 7) / 8 * 8;
   hipLaunchKernelGGL((tree_kernel<D, F8, PAGES16, CW, PARTS>), dim3((uint32_t)(pairs * s.blocks)), dim3(64 * kTreeWaves), LDS, stream, p, ws, s.blocks, s.shares,
                      s.direct ? 1 : 0);
@@ -231,8 +268,18 @@ hipError_t launch_columns(const TreeParams& p, const TreeShape& s, const TreeSpa
 }
 template <int D, bool F8, bool PAGES16>
 hipError_t launch_kernel(const TreeParams& p, const TreeShape& s, const TreeSpace& ws, hipStream_t stream) {
-  if (s.columns == 64) return launch_columns<D, F8, PAGES16, 2, 3>(p, s, ws, stream);
+  // P in bf16 where O is, or in three parts
+  if (s.columns == 64) return p.o.is_f32 ? launch_columns<D, F8, PAGES16, 2, 3>(p, s, ws, stream) : launch_columns<D, F8, PAGES16, 2, 1>(p, s, ws, stream);
   return p.o.is_f32 ? launch_columns<D, F8, PAGES16, 4, 3>(p, s, ws, stream) : launch_columns<D, F8, PAGES16, 4, 1>(p, s, ws, stream);
+}
+// Threads for the pieces of a sequence, of which it has as many as shares if it is the only long one.
+template <int D, int COLS>
+hipError_t launch_join(const TreeParams& p, const TreeShape& s, const TreeSpace& ws, hipStream_t stream) {
+  const int64_t rows = (int64_t)p.batch * p.sq * p.q_heads;
+  if (s.shares > 64 * p.batch) hipLaunchKernelGGL((tree_join_kernel<D, COLS, 16>), dim3((uint32_t)rows), dim3(16 * D / 4), 0, stream, p, ws, s.blocks);
+  else if (s.shares > 8 * p.batch) hipLaunchKernelGGL((tree_join_kernel<D, COLS, 4>), dim3((uint32_t)rows), dim3(4 * D / 4), 0, stream, p, ws, s.blocks);
+  else hipLaunchKernelGGL((tree_join_kernel<D, COLS, 1>), dim3((uint32_t)((rows * (D / 4) + 255) / 256)), dim3(256), 0, stream, p, ws, s.blocks);
+  return hipGetLastError();
 }
 template <int D, bool F8>
 hipError_t launch(const TreeParams& p, hipStream_t stream) {
@@ -240,14 +287,12 @@ hipError_t launch(const TreeParams& p, hipStream_t stream) {
   char* const space = (char*)p.workspace;
   const TreeSpace ws{(int2*)space, (float2*)(space + s.off_ml), (float*)(space + s.off_o)};
   hipError_t e;
-  if (s.columns == 32) e = launch_tree_few(p, ws, s.shares, s.direct, stream);
+  if (s.columns <= 32) e = launch_tree_few(p, ws, s.columns, s.shares, s.direct, stream);
   else e = p.cache.page_rows % 16 == 0 ? launch_kernel<D, F8, true>(p, s, ws, stream) : launch_kernel<D, F8, false>(p, s, ws, stream);
   if (e != hipSuccess || s.direct) return e;
-  const dim3 grid((uint32_t)(((int64_t)p.batch * p.sq * p.q_heads * (D / 4) + 255) / 256));
-  if (s.columns == 32) hipLaunchKernelGGL((tree_join_kernel<D, 32>), grid, dim3(256), 0, stream, p, ws, s.blocks);
-  else if (s.columns == 64) hipLaunchKernelGGL((tree_join_kernel<D, 64>), grid, dim3(256), 0, stream, p, ws, s.blocks);
-  else hipLaunchKernelGGL((tree_join_kernel<D, 128>), grid, dim3(256), 0, stream, p, ws, s.blocks);
-  return hipGetLastError();
+  if (s.columns == 16) return launch_join<D, 16>(p, s, ws, stream);
+  if (s.columns == 32) return launch_join<D, 32>(p, s, ws, stream);
+  return s.columns == 64 ? launch_join<D, 64>(p, s, ws, stream) : launch_join<D, 128>(p, s, ws, stream);
 }
 template <int D>
 hipError_t launch(const TreeParams& p, hipStream_t stream) {

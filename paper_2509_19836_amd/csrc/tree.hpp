@@ -249,20 +249,20 @@ struct TreeOperands {
   }
 };
 
-// 32 columns of a wave: column 16 nb + r of them is lane r's (and r + 16's, ..).  A column is a token and a query head; what it sees, its query,
+// 16 NB columns of a wave: column 16 nb + r of them is lane r's (and r + 16's, ..).  A column is a token and a query head; what it sees, its query,
 // its running maximum (base 2, a whole number, so that a rescale changes no bit of P and O) and sums.
-// PARTS: bf16 numbers that a P is multiplied in; AHEAD: operands fetched before they are used.
-template <int D, bool F8, int PARTS, int AHEAD>
+// PARTS: bf16 numbers that a P is multiplied in; AHEAD: operands fetched before they are used; CH: 32 rows at a time, or twice as many.
+template <int D, bool F8, int NB, int PARTS, int AHEAD, int CH>
 struct TreeColumns {
-  static constexpr int NB = 2, MB = 2, DK = D / 32, DB = D / 16;
+  static constexpr int MB = 2 * CH, DK = D / 32, DB = D / 16, HALF = TreeOperands<D, F8>::TILE;
   bf16x8 q[DK][NB];
   int32_t first[NB], latest, older, sinks;
   uint64_t word[NB];
   float to_log2, m[NB], l[NB];
   f32x4 acc[DB][NB], s[MB][NB];
-  bf16x8 part[NB][PARTS];
+  bf16x8 part[CH][NB][PARTS];
 
-  // Columns c0 .. c0 + 31 of `columns` (those behind are as if there were none: zeros)
+  // Columns from c0 on (those behind the sequence's last one are zeros)
   __device__ __forceinline__ void init(const TreeParams& p, const TreeSeq& seq, int32_t b, int32_t hk, int32_t group, int32_t c0, int lane) {
     const int r = lane & 15, g = lane >> 4;
     older = seq.older;
@@ -288,40 +288,40 @@ struct TreeColumns {
     latest = __builtin_amdgcn_readfirstlane(last);
     to_log2 = p.scale * kLog2e * (F8 && p.cache.k_scale ? p.cache.k_scale[hk] : 1.f);
   }
-  // Scores of the 32 rows whose keys lie in LDS at kt
+  // Scores of the rows whose keys lie in LDS at kt
   __device__ __forceinline__ void scores(uint32_t kt, const TreeOperands<D, F8>& ops) {
     constexpr int N = DK * MB;
     typename TreeOperands<D, F8>::Raw a[N];
     MatrixPhase prio;
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) a[i] = ops.row(kt, i % MB, i / MB);
+    for (int i = 0; i < AHEAD; ++i) a[i] = ops.row(kt + i % MB / 2 * HALF, i % 2, i / MB);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (i + AHEAD < N) a[i + AHEAD] = ops.row(kt, (i + AHEAD) % MB, (i + AHEAD) / MB);
+      if (i + AHEAD < N) a[i + AHEAD] = ops.row(kt + (i + AHEAD) % MB / 2 * HALF, (i + AHEAD) % 2, (i + AHEAD) / MB);
       const bf16x8 x = ops.wide(a[i]);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) s[i % MB][nb] = mfma16(x, q[i / MB][nb], i < MB ? f32x4{0.f, 0.f, 0.f, 0.f} : s[i % MB][nb]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // Whether every column sees all of the 32 rows from t0 on, if they are there
-  __device__ __forceinline__ bool sees_all(int32_t t0) const { return t0 + 32 <= older && (t0 >= latest || t0 + 32 <= sinks); }
+  // Whether every column sees all of the rows from t0 on, if they are there
+  __device__ __forceinline__ bool sees_all(int32_t t0) const { return t0 + 32 * CH <= older && (t0 >= latest || t0 + 32 * CH <= sinks); }
   // P of these rows (from t0 on; `there`: which of them are) as bf16 numbers that add up to it
-  __device__ __forceinline__ void weights(int32_t t0, uint32_t there, int g) {
-    const bool full = there == ~0u && sees_all(t0);   // (wave-uniform)
+  __device__ __forceinline__ void weights(int32_t t0, uint64_t there, int g) {
+    const bool full = there == low_bits(32 * CH) && sees_all(t0);   // (wave-uniform)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      float x[8], top = -INFINITY;
+      float x[8 * CH], top = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][nb][e & 3];
+      for (int e = 0; e < 8 * CH; ++e) x[e] = s[e >> 2][nb][e & 3];
       if (!full) {
-        const uint64_t sees = rows_between(first[nb], older, t0) | rows_between(0, sinks, t0) | moved(word[nb], older - t0);
-        const uint32_t bits = ((uint32_t)sees & there) >> (4 * g);
+        const uint64_t sees = (rows_between(first[nb], older, t0) | rows_between(0, sinks, t0) | moved(word[nb], older - t0)) & there;
+        const uint32_t bits[2] = {(uint32_t)sees >> (4 * g), (uint32_t)(sees >> 32) >> (4 * g)};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (bits >> (16 * (e >> 2) + (e & 3))) & 1 ? x[e] : -INFINITY;
+        for (int e = 0; e < 8 * CH; ++e) x[e] = (bits[e >> 3] >> (16 * ((e >> 2) & 1) + (e & 3))) & 1 ? x[e] : -INFINITY;
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
+      for (int e = 0; e < 8 * CH; ++e) top = fmaxf(top, x[e]);
       top *= to_log2;   // (positive)
       if (__any(top > m[nb] + kTreeStale)) {   // (the first rows: m is -inf)
         top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -334,13 +334,16 @@ struct TreeColumns {
       }
       const float base = m[nb] == -INFINITY ? 0.f : m[nb];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], to_log2, -base));
-        l[nb] += x[e];
+      for (int c = 0; c < CH; ++c) {
+        float* const y = x + 8 * c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_exp2f(fmaf(y[e], to_log2, -base));
+        l[nb] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+        if constexpr (PARTS == 1) part[c][nb][0] = pack_pair(f32x4{y[0], y[1], y[2], y[3]}, f32x4{y[4], y[5], y[6], y[7]});
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (PARTS == 1) {
-        part[nb][0] = pack_pair(f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]});
-      } else {
+      if constexpr (PARTS > 1) {
+        static_assert(PARTS == 1 || CH == 1, "registers");
         u16x2 least[4];
 #pragma unroll
         for (int n = 0; n < PARTS; ++n) {
@@ -356,26 +359,27 @@ struct TreeColumns {
             x0 -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x0) & 0xffff0000u);   // (exact)
             x1 -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x1) & 0xffff0000u);
           }
-          part[nb][n] = __builtin_bit_cast(bf16x8, words);
+          part[0][nb][n] = __builtin_bit_cast(bf16x8, words);
         }
       }
       __builtin_amdgcn_sched_barrier(0);   // (one block of columns after the other: both at once take the registers of twice as many numbers)
     }
   }
-  // O += V^T P, with the values of the 32 rows in LDS at vt
+  // O += V^T P, with the values of the rows in LDS at vt
   __device__ __forceinline__ void add(uint32_t vt, const TreeOperands<D, F8>& ops) {
-    typename TreeOperands<D, F8>::Raw a[DB];
+    constexpr int N = CH * DB;
+    typename TreeOperands<D, F8>::Raw a[N];
     MatrixPhase prio;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) a[i] = ops.col(vt, i);
 #pragma unroll
-    for (int i = 0; i < DB; ++i) {
-      if (i + AHEAD < DB) a[i + AHEAD] = ops.col(vt, i + AHEAD);
+    for (int i = 0; i < N; ++i) {
+      if (i + AHEAD < N) a[i + AHEAD] = ops.col(vt + (i + AHEAD) / DB * HALF, (i + AHEAD) % DB);
       const bf16x8 v = ops.wide(a[i]);
 #pragma unroll
       for (int n = 0; n < PARTS; ++n)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) acc[i][nb] = mfma16(v, part[nb][n], acc[i][nb]);
+        for (int nb = 0; nb < NB; ++nb) acc[i % DB][nb] = mfma16(v, part[i / DB][nb][n], acc[i % DB][nb]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -525,6 +529,6 @@ struct TreeRun {
   }
 };
 
-hipError_t launch_tree_few(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream);
+hipError_t launch_tree_few(const TreeParams& p, const TreeSpace& ws, int32_t columns, int32_t shares, bool direct, hipStream_t stream);
 
 }  // namespace burst

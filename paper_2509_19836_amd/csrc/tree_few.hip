@@ -8,15 +8,17 @@ namespace burst {
 
 namespace {
 
-// NW: waves of a work-group, four where rows are dealt to many, eight where a work-group has a whole sequence.
-template <int D, bool F8, bool PAGES16, int NW>
+constexpr int few_slots(int head_dim, bool f8) { return (1 << 14) / (2 * 32 * head_dim * (f8 ? 1 : 2)); }   // 16 KiB a wave
+
+// NB: blocks of 16 columns.  NW: waves of a work-group, four where rows are dealt to many, eight where a work-group has a whole sequence.
+template <int D, bool F8, bool PAGES16, int NB, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void tree_few_kernel(TreeParams, TreeSpace ws, int32_t shares, int32_t direct) {
-  using Columns = TreeColumns<D, F8, 3, D == 128 && !F8 && !PAGES16 ? 1 : 4>;   // (registers)
+  using Columns = TreeColumns<D, F8, NB, 3, D == 128 && !F8 && !PAGES16 && NB == 2 ? 1 : 4, 1>;   // (registers)
   using Run = TreeRun<D, F8, PAGES16, 2>;
   using Operands = TreeOperands<D, F8>;
-  constexpr int NB = Columns::NB, DB = Columns::DB, UNIT = 32 * NW, TILE = Operands::TILE, NI = Run::NI;
-  constexpr int SLOTS = F8 ? 2 : 1, LOADS = 2 * NI * (2 * SLOTS - 1);   // tiles under way; loads behind those that a product waits for
-  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [wave][slot][K tile, V tile], maxima and sums [wave][32]
+  constexpr int DB = Columns::DB, UNIT = 32 * NW, TILE = Operands::TILE, NI = Run::NI;
+  constexpr int SLOTS = few_slots(D, F8), LOADS = 2 * NI * (2 * SLOTS - 1);   // tiles under way; loads behind those that a product waits for
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [wave][slot][K tile, V tile], maxima and sums [wave][16 NB]
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, g = lane >> 4;
   char* const tiles = smem + wave * SLOTS * 2 * TILE;
   const uint32_t tiles0 = (uint32_t)(uintptr_t)(lds_bytes)tiles;
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_few_kernel(TreeParams, TreeSp
       for (int h = 0; h < 2; ++h) Run::clear(tiles + (slot * 2 + 1) * TILE + Run::BYTES * h, (now >> (16 * h)) & 0xffffu, lane);
       x.add(vt, ops);
       if (more) ask_v(vt);
-      if (SLOTS == 2) slot ^= 1;
+      slot = (slot + 1) & (SLOTS - 1);
     }
     x.finish();
     const TreeParams& p = args_here();
@@ -105,31 +107,32 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_few_kernel(TreeParams, TreeSp
     // The waves' sums against their largest maximum; where their tiles were
     if (g == 0) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) ml_lds[32 * wave + 16 * nb + r] = float2{x.m[nb], x.l[nb]};
+      for (int nb = 0; nb < NB; ++nb) ml_lds[16 * NB * wave + 16 * nb + r] = float2{x.m[nb], x.l[nb]};
     }
     f32x4* const sums = reinterpret_cast<f32x4*>(smem);   // [wave][block of 16 elements][column block][lane]
-    static_assert(DB * NB * 64 * 16 == SLOTS * 2 * TILE, "a wave's sums fit where its tiles were");
+    constexpr int PITCH = SLOTS * 2 * TILE / 16;
+    static_assert(DB * NB * 64 <= PITCH, "a wave's sums fit where its tiles were");
 #pragma unroll
-    for (int i = 0; i < DB * NB; ++i) sums[(wave * DB * NB + i) * 64 + lane] = x.acc[i / NB][i % NB];
+    for (int i = 0; i < DB * NB; ++i) sums[wave * PITCH + i * 64 + lane] = x.acc[i / NB][i % NB];
     __syncthreads();
     for (int i = tid; i < DB * NB * 64; i += 64 * NW) {
       const int at = i / 64, l = i % 64, nb = at % NB, c = 16 * nb + l % 16, d = 16 * (at / NB) + 4 * (l / 16);
       if (c >= columns) continue;
       float top = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) top = fmaxf(top, ml_lds[32 * w + c].x);
+      for (int w = 0; w < NW; ++w) top = fmaxf(top, ml_lds[16 * NB * w + c].x);
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        const float2 ml = ml_lds[32 * w + c];
+        const float2 ml = ml_lds[16 * NB * w + c];
         const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
         sum += ml.y * f;
-        o += sums[(w * DB * NB + at) * 64 + l] * f;
+        o += sums[w * PITCH + at * 64 + l] * f;
       }
       if (walk.whole) {
         tree_write<F8>(p, b, hk, group, c, d, o, top, sum);
       } else {
-        const int64_t piece = (2 * ((int64_t)share * kv_heads + hk) + (walk.first_piece ? 0 : 1)) * 32 + c;
+        const int64_t piece = (2 * ((int64_t)share * kv_heads + hk) + (walk.first_piece ? 0 : 1)) * (16 * NB) + c;
         *reinterpret_cast<f32x4*>(ws.o + piece * D + d) = o;
         if (d == 0) ws.ml[piece] = float2{top, sum};
       }
@@ -138,24 +141,27 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_few_kernel(TreeParams, TreeSp
   } while (walk.next(args_here(), direct != 0));
 }
 
-template <int D, bool F8, bool PAGES16, int NW>
-hipError_t launch(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream) {
-  constexpr int LDS = NW * (32 * 4 * D + 32 * 8);   // (tiles of e4m3 are half as large and twice as many)
-  hipLaunchKernelGGL((tree_few_kernel<D, F8, PAGES16, NW>), dim3((uint32_t)((int64_t)shares * p.kv_heads)), dim3(64 * NW), LDS, stream, p, ws, shares, direct ? 1 : 0);
+template <int D, bool F8, bool PAGES16, int NB, int NW>
+hipError_t launch_kernel(const TreeParams& p, const TreeSpace& ws, int32_t shares, hipStream_t stream) {
+  constexpr int LDS = NW * ((1 << 14) + 16 * NB * 8);
+  hipLaunchKernelGGL((tree_few_kernel<D, F8, PAGES16, NB, NW>), dim3((uint32_t)((int64_t)shares * p.kv_heads)), dim3(64 * NW), LDS, stream, p, ws, shares, NW == 8 ? 1 : 0);
   return hipGetLastError();
 }
+template <int D, bool F8, bool PAGES16>
+hipError_t launch(const TreeParams& p, const TreeSpace& ws, int32_t columns, int32_t shares, bool direct, hipStream_t stream) {
+  if (columns == 16) return direct ? launch_kernel<D, F8, PAGES16, 1, 8>(p, ws, shares, stream) : launch_kernel<D, F8, PAGES16, 1, 4>(p, ws, shares, stream);
+  return direct ? launch_kernel<D, F8, PAGES16, 2, 8>(p, ws, shares, stream) : launch_kernel<D, F8, PAGES16, 2, 4>(p, ws, shares, stream);
+}
 template <int D, bool F8>
-hipError_t launch(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream) {
-  const bool pages16 = p.cache.page_rows % 16 == 0;
-  if (direct) return pages16 ? launch<D, F8, true, 8>(p, ws, shares, true, stream) : launch<D, F8, false, 8>(p, ws, shares, true, stream);
-  return pages16 ? launch<D, F8, true, 4>(p, ws, shares, false, stream) : launch<D, F8, false, 4>(p, ws, shares, false, stream);
+hipError_t launch(const TreeParams& p, const TreeSpace& ws, int32_t columns, int32_t shares, bool direct, hipStream_t stream) {
+  return p.cache.page_rows % 16 == 0 ? launch<D, F8, true>(p, ws, columns, shares, direct, stream) : launch<D, F8, false>(p, ws, columns, shares, direct, stream);
 }
 
 }  // namespace
 
-hipError_t launch_tree_few(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream) {
-  if (p.head_dim == 128) return p.cache.is_f8 ? launch<128, true>(p, ws, shares, direct, stream) : launch<128, false>(p, ws, shares, direct, stream);
-  return p.cache.is_f8 ? launch<64, true>(p, ws, shares, direct, stream) : launch<64, false>(p, ws, shares, direct, stream);
+hipError_t launch_tree_few(const TreeParams& p, const TreeSpace& ws, int32_t columns, int32_t shares, bool direct, hipStream_t stream) {
+  if (p.head_dim == 128) return p.cache.is_f8 ? launch<128, true>(p, ws, columns, shares, direct, stream) : launch<128, false>(p, ws, columns, shares, direct, stream);
+  return p.cache.is_f8 ? launch<64, true>(p, ws, columns, shares, direct, stream) : launch<64, false>(p, ws, columns, shares, direct, stream);
 }
 
 }  // namespace burst

@@ -3,7 +3,7 @@
 Tolerances, with u = 2^-24 and A the largest sum of |q| |K| of a token's head times the scale, as for one new token: a score is a sum of head_dim exact
 products in fp32, off by at most head_dim u A, and its conversion to base 2 by 4 u A: e = (head_dim + 4) u A.  Lse is off by at most e, (n + 16) u for the
 sum of n numbers, exponential and logarithm, and 4 u of its own size.  O, whose numbers P go in whole (to 2^-30 of each), by (2 e + (n + 16) u + 2^-30)
-sum P |V|; in bf16 the result is rounded by half a step, 2^-8 of it, and with more than 64 columns (tokens times query heads of a key head) so is each P."""
+sum P |V|; in bf16 the result is rounded by half a step, 2^-8 of it, and with more than 32 columns (tokens times query heads of a key head) so is each P."""
 import math
 
 import numpy as np
@@ -106,7 +106,7 @@ def test_tree_against_the_reference(lib, case):
     ref = reference(P, q_host, tokens, d ** -0.5, seen=seen)
     for max_rows in sorted({max(rows), P.table.shape[1] * page_rows}):
         o, lse = run_tree(lib, P, q, d ** -0.5, max_rows, tokens, seen, o_type=o_type)
-        check_tree(o, lse, ref, max(rows), d, o_type == "bf16", sq * Hq // Hkv > 64)
+        check_tree(o, lse, ref, max(rows), d, o_type == "bf16", sq * Hq // Hkv > 32)
     o2, _ = run_tree(lib, P, q, d ** -0.5, max_rows, tokens, seen, o_type=o_type, want_lse=False)
     assert o.equal(o2)                                                         # the same call, the same bits, with Lse and without
 
@@ -296,11 +296,11 @@ def test_scan_over_the_sequences(lib, B, group):
 
 
 def test_every_way_of_dealing(lib):
-    """Direct and dealt, 32, 64 and 128 columns, blocks that only longer sequences have, by burst_attn_tree_plan."""
+    """Direct and dealt, 16 to 128 columns, blocks that only longer sequences have, by burst_attn_tree_plan."""
     rng = np.random.Generator(np.random.PCG64(wl.BASE_SEED + 91100))
-    for B, Hkv, sq, Hq, longest, columns, direct in ((3, 2, 8, 8, 1500, 32, False), (3, 2, 8, 8, 100, 32, True), (3, 2, 16, 8, 1500, 64, False), (3, 2, 16, 8, 200, 64, True),
-                                                     (2, 2, 40, 8, 1500, 128, False), (70, 8, 2, 8, 3000, 32, True), (70, 8, 50, 8, 900, 64, True),
-                                                     (70, 4, 64, 16, 300, 128, True)):
+    for B, Hkv, sq, Hq, longest, columns, direct in ((3, 2, 8, 8, 1500, 32, False), (3, 2, 8, 8, 100, 32, True), (3, 2, 4, 8, 1500, 16, False), (3, 2, 3, 8, 300, 16, True), (3, 2, 16, 8, 1500, 64, False), (3, 2, 16, 8, 200, 64, True),
+                                                     (2, 2, 30, 8, 1500, 128, False), (2, 2, 40, 8, 1500, 128, False), (70, 8, 20, 8, 3000, 32, True), (70, 8, 2, 8, 3000, 16, True), (70, 8, 50, 8, 900, 64, True),
+                                                     (130, 4, 30, 16, 300, 128, True), (70, 4, 64, 16, 300, 128, True)):
         assert lib.burst_attn_tree_plan(lib.shape(B, Hq, Hkv, 64, sq, longest, 1.0))[1:] == (columns, direct)
         rows = rng.integers(sq, longest, B).tolist()
         rows[0] = longest
