@@ -3,13 +3,14 @@
 // Every logit is read once.  With x the logits times scale, m their maximum, l = sum exp(x - m) and w = sum exp(x - m) (x - m):
 //     lse = m + log l,   logp = x_y - lse,   entropy = log l - w / l   (in base 2 inside),
 // kept against a running maximum by each lane of its own elements.
-//   The likeliest words: a wave has a list of 64, one a lane, in order.  The list starts from each lane's best element of the wave's first step, so its n_top-th
-// is a bound that about n_top elements of that step pass; of each later step only what passes the bound is looked at (one comparison of a lane's
-// maximum, which the sum needs anyway, for 8 or 4 elements), gathered in LDS, and taken into the list 64 at a time by a bitonic sort and merge.  An entry is
-// the number, as a whole one of the same order, over the complement of its index: equal numbers go by the lowest index, and any way of dealing the
-// elements out gives the same list.
+//   The likeliest words: while the row is read, each lane keeps the largest number of its elements, the step (32 or 16 elements) where it came first, and the
+// largest of the other steps: nine instructions a step.  The n_top-th of the lanes' largest is a bound that n_top words reach, and only those n_top lanes
+// can have others: they read that step again (and, the few whose second largest reaches the bound, the others), and what reaches the bound, about n_top words,
+// is sorted.  An entry is the number, as a whole one of the same order, over the complement of its index: equal numbers go by the lowest index, rows of equal
+// numbers (masked ones) give a bound that few words reach like any other, and any way of dealing the elements out gives the same words.
 //   A row is a wave's where there are many, else several waves' or several work-groups', whose sums and lists are joined.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.hpp"
 #include "kernels.hpp"
@@ -21,6 +22,7 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) float f32x8;
 
 constexpr int kMostSegments = 16;      // work-groups of a row
+constexpr int64_t kScoresUnits = 256;   // compute units
 constexpr float kNothing = -1000.f;    // exp2 of this is 0: in place of -inf where it is multiplied with such a zero
 
 // A number and its index as one whole number: greater numbers first, among equals (0 and -0 are) the lower index.  0: no entry.
@@ -36,24 +38,43 @@ __device__ __forceinline__ float number_of(uint64_t entry) {
 }
 __device__ __forceinline__ bool is_nan(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7fffffffu) > 0x7f800000u; }
 
-// One stage of a bitonic network over the lanes: of the two lanes that `step` parts, the one below keeps the larger if `larger_below`.
-__device__ __forceinline__ uint64_t exchanged(uint64_t x, int step, bool larger_below, int lane) {
-  const uint64_t y = __shfl_xor((unsigned long long)x, step, 64);
-  return (x > y) == (((lane & step) == 0) == larger_below) ? x : y;
+// The value of the lane that differs by STEP.  By the vector unit's own moves, not through LDS: a stage of the networks below in a quarter of the time.
+template <int STEP>
+__device__ __forceinline__ uint32_t of_lane_xor(uint32_t x) {
+  if constexpr (STEP == 1) return __builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, false);         // quad_perm [1, 0, 3, 2]
+  else if constexpr (STEP == 2) return __builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, false);    // quad_perm [2, 3, 0, 1]
+  else if constexpr (STEP == 4) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, false), 0x1b, 0xf, 0xf, false);   // 8 lanes, then 4, the other way round
+  else if constexpr (STEP == 8) return __builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, false);   // row_ror 8
+  else if constexpr (STEP == 16) {
+    const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return (threadIdx.x & 16) ? y[0] : y[1];
+  } else {
+    const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return (threadIdx.x & 32) ? y[0] : y[1];
+  }
+}
+// One stage of a bitonic network over the lanes: of the two lanes that STEP parts, the one below keeps the larger if `larger_below`.
+template <int STEP>
+__device__ __forceinline__ uint64_t exchanged(uint64_t x, bool larger_below, int lane) {
+  const uint64_t y = (uint64_t)of_lane_xor<STEP>((uint32_t)(x >> 32)) << 32 | of_lane_xor<STEP>((uint32_t)x);
+  return (x > y) == (((lane & STEP) == 0) == larger_below) ? x : y;
+}
+template <int STEP>
+__device__ __forceinline__ uint64_t exchanged_down(uint64_t x, bool larger_below, int lane) {   // stages STEP, STEP / 2, .. 1
+  x = exchanged<STEP>(x, larger_below, lane);
+  if constexpr (STEP > 1) x = exchanged_down<STEP / 2>(x, larger_below, lane);
+  return x;
 }
 // A bitonic sequence sorted, the largest in lane 0
-__device__ __forceinline__ uint64_t merged_down(uint64_t x, int lane) {
-#pragma unroll
-  for (int step = 32; step >= 1; step >>= 1) x = exchanged(x, step, true, lane);
-  return x;
-}
+__device__ __forceinline__ uint64_t merged_down(uint64_t x, int lane) { return exchanged_down<32>(x, true, lane); }
 template <bool DOWN>
 __device__ __forceinline__ uint64_t sorted(uint64_t x, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-    for (int step = size >> 1; step >= 1; step >>= 1) x = exchanged(x, step, ((lane & size) == 0 || size == 64) == DOWN, lane);
-  return x;
+  x = exchanged_down<1>(x, ((lane & 2) == 0) == DOWN, lane);
+  x = exchanged_down<2>(x, ((lane & 4) == 0) == DOWN, lane);
+  x = exchanged_down<4>(x, ((lane & 8) == 0) == DOWN, lane);
+  x = exchanged_down<8>(x, ((lane & 16) == 0) == DOWN, lane);
+  x = exchanged_down<16>(x, ((lane & 32) == 0) == DOWN, lane);
+  return exchanged_down<32>(x, DOWN, lane);
 }
 // The 64 largest of a list and of entries sorted the other way round
 __device__ __forceinline__ uint64_t joined(uint64_t list, uint64_t up, int lane) { return merged_down(list > up ? list : up, lane); }
@@ -69,9 +90,18 @@ struct RowSums {
     l = l * f0 + o.l * f1;
     m = top;
   }
+  template <int STEP>
+  __device__ __forceinline__ void join_lane_xor() {
+    auto other = [](float x) { return __builtin_bit_cast(float, of_lane_xor<STEP>(__builtin_bit_cast(uint32_t, x))); };
+    join(RowSums{other(m), other(l), other(w)});
+  }
   __device__ __forceinline__ void join_lanes() {
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) join(RowSums{__shfl_xor(m, s, 64), __shfl_xor(l, s, 64), __shfl_xor(w, s, 64)});
+    join_lane_xor<1>();
+    join_lane_xor<2>();
+    join_lane_xor<4>();
+    join_lane_xor<8>();
+    join_lane_xor<16>();
+    join_lane_xor<32>();
   }
 };
 
@@ -114,137 +144,79 @@ struct RowVectors {
   }
 };
 
-// The list of a wave's likeliest words.
-struct TopList {
-  uint64_t list;       // a lane's entry, the largest in lane 0
-  uint64_t bound;      // the n_top-th
-  float bound_number;
-  uint64_t* pending;   // LDS of the wave: fewer than 64, and what one vector of each lane may add
-  int count, n_top, lane;
-  __device__ __forceinline__ void set_bound() {
-    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)list, n_top - 1), hi = __builtin_amdgcn_readlane((uint32_t)(list >> 32), n_top - 1);
-    bound = (uint64_t)hi << 32 | lo;
-    bound_number = number_of(bound);
-  }
-  __device__ __forceinline__ void start(uint64_t best, uint64_t* lds, int n, int lane_) {
-    pending = lds;
-    n_top = n;
-    lane = lane_;
-    count = 0;
-    list = sorted<true>(best, lane);
-    set_bound();
-  }
-  __device__ __forceinline__ void offer(uint64_t entry, bool is_new) {
-    const uint64_t passes = __ballot(is_new && entry > bound);
-    if (passes == 0) return;
-    if ((passes >> lane) & 1) pending[count + __builtin_popcountll(passes & ((1ull << lane) - 1))] = entry;
-    count += __builtin_popcountll(passes);
-  }
-  // What is pending goes into the list, 64 at a time, until fewer than `rest` are left
-  __device__ __forceinline__ void take(int rest) {
-    int head = 0;
-    __builtin_amdgcn_wave_barrier();
-    while (count - head >= rest) {
-      const uint64_t x = head + lane < count ? pending[head + lane] : 0;
-      list = joined(list, sorted<false>(x, lane), lane);
-      head += 64;
-    }
-    if (head == 0) return;
-    set_bound();
-    count = count > head ? count - head : 0;
-    const uint64_t x = lane < count ? pending[head + lane] : 0;
-    __builtin_amdgcn_wave_barrier();
-    if (lane < count) pending[lane] = x;
-    __builtin_amdgcn_wave_barrier();
+// What a lane remembers of its part of a row: the largest numbers of the steps where they are largest and next to largest, those steps (their first vector;
+// among equals the first step), and the largest number of all others.
+struct LaneBest {
+  float best, second, third;
+  int32_t step, second_step;
+  __device__ __forceinline__ void see(float x, int32_t j0) {
+    const bool first = x > best, next = x > second;
+    third = fmaxf(third, fminf(second, x));
+    second_step = first ? step : next ? j0 : second_step;
+    second = fmaxf(second, fminf(best, x));
+    step = first ? j0 : step;
+    best = fmaxf(best, x);
   }
 };
 
-constexpr int kPending = 64 + 64 * 8;   // entries in LDS of a wave
-
-// A wave's part of a row, vectors v0 .. v1 - 1.
+// A wave's part of a row, vectors v0 .. v1 - 1, 64 U in each step.
+constexpr int U = 4;
 template <bool F32, bool TOP>
-__device__ __forceinline__ void scan_row(const RowVectors<F32>& row, int32_t v0, int32_t v1, float to_log2, int n_top, uint64_t* pending, int lane,
-                                         RowSums& sums, uint64_t& list) {
-  constexpr int VEC = RowVectors<F32>::VEC, U = 4;
+__device__ __forceinline__ void scan_row(const RowVectors<F32>& row, int32_t v0, int32_t v1, float to_log2, int lane, RowSums& sums, LaneBest& top) {
+  constexpr int VEC = RowVectors<F32>::VEC;
   sums = RowSums{-INFINITY, 0.f, 0.f};
-  TopList top;
-  top.list = 0;
-  auto index = [&](int32_t j, int i) { return (int32_t)((int64_t)j * VEC - row.before + i); };
-  auto is_word = [&](int32_t id, float y) { return id >= 0 && id < row.vocab && !is_nan(y); };
-  uint64_t best = 0;   // what the list starts from is not offered again
-  if (TOP && v0 < v1) {
-#pragma clang loop unroll(disable)
-    for (int32_t j = v0 + lane; j < min(v1, v0 + 64 * U); j += 64) {
-      const u32x4 x = row.load(j);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float y = RowVectors<F32>::value(x, i);
-        const uint64_t entry = is_word(index(j, i), y) ? entry_of(y, index(j, i)) : 0;
-        best = entry > best ? entry : best;
-      }
-    }
-    top.start(best, pending, n_top, lane);
-  }
+  top = LaneBest{-INFINITY, -INFINITY, -INFINITY, v0, v0};
+  bool masked = false;   // some number so far was -inf (or NaN)
   for (int32_t j0 = v0; j0 < v1; j0 += 64 * U) {
     u32x4 x[U];
     const u32x4 none = F32 ? u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u} : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
 #pragma unroll
     for (int u = 0; u < U; ++u) x[u] = j0 + 64 * u + lane < v1 ? row.load(j0 + 64 * u + lane) : none;
-    float most[U], step = -INFINITY;
+    float most[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      most[u] = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) most[u] = fmaxf(most[u], RowVectors<F32>::value(x[u], i));
-      step = fmaxf(step, most[u]);
+      auto y = [&](int i) { return RowVectors<F32>::value(x[u], i); };
+      most[u] = max3(y(0), y(1), max3(y(2), y(3), -INFINITY));
+      if constexpr (!F32) most[u] = max3(max3(y(4), y(5), most[u]), y(6), y(7));
     }
+    static_assert(U == 4, "four of them");
+    const float step = max3(max3(most[0], most[1], most[2]), most[3], -INFINITY);
+    if constexpr (TOP) top.see(step, j0);
     // (a scale is positive: the largest logit is the largest exponent)
     const float m = fmaxf(sums.m, step * to_log2), d = sums.m == m ? 0.f : fmaxf(sums.m - m, kNothing), f = __builtin_amdgcn_exp2f(d);
     sums.w = (sums.w + sums.l * d) * f;
     sums.l *= f;
     sums.m = m;
     const float base = m == -INFINITY ? 0.f : m;
+    auto add = [&](auto masked_) {   // (a number at -inf has the weight 0, and 0 * -inf would be NaN)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float e = fmaf(RowVectors<F32>::value(x[u], i), to_log2, -base), p = __builtin_amdgcn_exp2f(e);
-        sums.l += p;
-        sums.w = fmaf(p, fmaxf(e, kNothing), sums.w);
-      }
-    if constexpr (TOP) {
-      uint32_t some = 0;
-#pragma unroll
-      for (int u = 0; u < U; ++u) some |= __any(most[u] >= top.bound_number) ? 1u << u : 0u;
-      while (some != 0) {   // (the vector is read again: a copy of this for each of them would cost the registers of all)
-        const int u = __builtin_ctz(some);
-        some &= some - 1;
-        const bool inside = j0 + 64 * u + lane < v1;
-        const u32x4 again = inside ? row.load(j0 + 64 * u + lane) : none;
+      for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          const float y = RowVectors<F32>::value(again, i);
-          const int32_t id = index(j0 + 64 * u + lane, i);
-          const uint64_t entry = entry_of(y, id);
-          top.offer(entry, inside && is_word(id, y) && entry != best);
+          const float e = fmaf(RowVectors<F32>::value(x[u], i), to_log2, -base), p = __builtin_amdgcn_exp2f(e);
+          sums.l += p;
+          sums.w = fmaf(p, decltype(masked_)::value ? fmaxf(e, kNothing) : e, sums.w);
         }
-        top.take(64);
+    };
+    if (!masked) {   // without that care as long as there is none
+      const float l = sums.l, w = sums.w;
+      add(std::false_type());
+      masked = __any(is_nan(sums.w)) != 0;
+      if (masked) {
+        sums.l = l;
+        sums.w = w;
       }
     }
-  }
-  if constexpr (TOP) {
-    if (v0 < v1) top.take(1);
-    list = top.list;
+    if (masked) add(std::true_type());
   }
   sums.join_lanes();
 }
 
 // Sums and lists of the work-group's waves, in wave 0.
-// lists: PITCH entries of LDS for each wave, the first 64 of them used.
-template <int W, bool TOP, int PITCH>
+template <int W, bool TOP>
 __device__ __forceinline__ void join_waves(RowSums& sums, uint64_t& list, RowSums* sums_lds, uint64_t* lists, int wave, int lane) {
   if (lane == 0) sums_lds[wave] = sums;
-  if (TOP) lists[PITCH * wave + lane] = list;
+  if (TOP) lists[64 * wave + lane] = list;
   __syncthreads();
 #pragma unroll
   for (int s = 1; s < W; s <<= 1) {
@@ -252,12 +224,133 @@ __device__ __forceinline__ void join_waves(RowSums& sums, uint64_t& list, RowSum
       sums.join(sums_lds[wave + s]);
       if (lane == 0) sums_lds[wave] = sums;
       if (TOP) {
-        list = joined(list, lists[PITCH * (wave + s) + 63 - lane], lane);
-        lists[PITCH * wave + lane] = list;
+        list = joined(list, lists[64 * (wave + s) + 63 - lane], lane);
+        lists[64 * wave + lane] = list;
       }
     }
     __syncthreads();
   }
+}
+// A lane's entry, in all of them
+__device__ __forceinline__ uint64_t of_lane(uint64_t x, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+
+// The likeliest words of a part of a row that W waves have, vectors v0 .. v1 - 1 this one: a lane each of wave 0, the first in lane 0.  found: LDS, kFound entries
+// and behind them their number (zero), of the waves together; lists: as for join_waves.  sums are joined on the way.
+template <int W>
+constexpr int kFound = W == 1 ? 256 : 1024;
+template <bool F32, int W>
+__device__ __forceinline__ uint64_t likeliest(const RowVectors<F32>& row, int32_t v0, int32_t v1, const LaneBest& top, int n_top, RowSums& sums, RowSums* sums_lds,
+                                              uint64_t* lists, uint64_t* found, int* count, int wave, int lane) {
+  constexpr int VEC = RowVectors<F32>::VEC;
+  auto index = [&](int32_t j, int i) { return (int32_t)((int64_t)j * VEC - row.before + i); };
+  auto is_word = [&](int32_t id, float y) { return (uint32_t)id < (uint32_t)row.vocab && !is_nan(y); };
+  // The step with the lane's largest number again, and the first word there that has it
+  u32x4 x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) x[u] = top.step + 64 * u + lane < v1 ? row.load(top.step + 64 * u + lane) : u32x4{};
+  uint64_t mine = 0;
+#pragma unroll
+  for (int u = U - 1; u >= 0; --u) {
+    const int32_t j = top.step + 64 * u + lane;
+    int32_t id = -1;
+#pragma unroll
+    for (int i = VEC - 1; i >= 0; --i) id = RowVectors<F32>::value(x[u], i) == top.best && (uint32_t)index(j, i) < (uint32_t)row.vocab ? index(j, i) : id;
+    mine = id >= 0 && j < v1 ? entry_of(top.best, id) : mine;
+  }
+  uint64_t list = sorted<true>(mine, lane);
+  uint64_t bound;
+  if constexpr (W == 1) {
+    bound = of_lane(list, n_top - 1);
+  } else {
+    join_waves<W, true>(sums, list, sums_lds, lists, wave, lane);
+    bound = lists[n_top - 1];
+  }
+  // What reaches it
+  const float bound_number = number_of(bound);
+  int n = 0;   // W = 1: found so far
+  auto look = [&](const u32x4& x, int32_t j, bool active) {
+    auto value = [&](int i) { return RowVectors<F32>::value(x, i); };
+    float most = max3(value(0), value(1), max3(value(2), value(3), -INFINITY));
+    if constexpr (!F32) most = max3(max3(value(4), value(5), most), value(6), value(7));
+    if (!__any(active && most >= bound_number)) return;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const float y = value(i);
+      const bool near = active && y >= bound_number;
+      if (!__any(near)) continue;
+      const uint64_t entry = entry_of(y, index(j, i));
+      const bool passes = near && is_word(index(j, i), y) && entry >= bound;
+      const uint64_t who = __ballot(passes);
+      if (who == 0) continue;
+      int at = n;
+      if constexpr (W == 1) n += __builtin_popcountll(who);
+      else at = __builtin_amdgcn_readlane(lane == __builtin_ctzll(who) ? atomicAdd(count, __builtin_popcountll(who)) : 0, __builtin_ctzll(who));
+      at += __builtin_popcountll(who & ((1ull << lane) - 1));
+      if (passes && at < kFound<W>) found[at] = entry;
+    }
+  };
+  const bool has = mine != 0 && mine >= bound;
+  if (__any(has)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) look(x[u], top.step + 64 * u + lane, has && top.step + 64 * u + lane < v1);
+  }
+  // (the step that a lane's second largest is from; it is the step above where there is no other, or nothing larger than -inf in it)
+  const bool second = has && top.second >= bound_number && top.second_step != top.step;
+  if (__any(second)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = second && top.second_step + 64 * u + lane < v1 ? row.load(top.second_step + 64 * u + lane) : u32x4{};
+#pragma unroll
+    for (int u = 0; u < U; ++u) look(x[u], top.second_step + 64 * u + lane, second && top.second_step + 64 * u + lane < v1);
+  }
+  const bool more = has && top.third >= bound_number;
+  if (__any(more)) {
+    for (int32_t j = v0; j < v1; j += 64 * U) {
+      const bool other = more && j != top.step && j != top.second_step;
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = other && j + 64 * u + lane < v1 ? row.load(j + 64 * u + lane) : u32x4{};
+#pragma unroll
+      for (int u = 0; u < U; ++u) look(x[u], j + 64 * u + lane, other && j + 64 * u + lane < v1);
+    }
+  }
+  if constexpr (W > 1) {
+    __syncthreads();
+    n = *count;
+  }
+  if (n <= kFound<W>) {
+    if (W > 1 && wave != 0) return 0;
+    __builtin_amdgcn_wave_barrier();
+    list = sorted<true>(lane < n ? found[lane] : 0, lane);
+    for (int c = 64; c < n; c += 64) list = joined(list, sorted<false>(c + lane < n ? found[c + lane] : 0, lane), lane);
+    return list;
+  }
+  // Too many (large numbers of which few lanes have all): the next one after the other, over the whole part each time
+  uint64_t last = ~0ull;
+  list = 0;
+  for (int t = 0; t < n_top; ++t) {
+    uint64_t next = 0;
+    for (int32_t j = v0 + lane; j < v1; j += 64) {
+      const u32x4 x = row.load(j);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float y = RowVectors<F32>::value(x, i);
+        const uint64_t entry = is_word(index(j, i), y) ? entry_of(y, index(j, i)) : 0;
+        if (entry < last && entry > next) next = entry;
+      }
+    }
+    next = of_lane(sorted<true>(next, lane), 0);
+    if constexpr (W > 1) {
+      __syncthreads();
+      if (lane == 0) found[wave] = next;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < W; ++w) next = found[w] > next ? found[w] : next;
+    }
+    if (lane == t) list = next;
+    last = next;
+  }
+  return list;
 }
 
 // A token's results from its row's sums and list, by one wave.
@@ -292,20 +385,25 @@ struct Partial {
 template <bool F32, bool TOP, int W>
 __global__ __launch_bounds__(64 * (W == 1 ? 4 : W)) void scores_kernel(ScoresParams p, int32_t segments) {
   constexpr int WAVES = W == 1 ? 4 : W;
-  __shared__ uint64_t pending[TOP ? WAVES : 1][kPending];
+  __shared__ uint64_t lists[TOP && W > 1 ? W * 64 : 1];
+  __shared__ uint64_t found[W == 1 ? WAVES : 1][TOP ? kFound<W> : 1];
   __shared__ RowSums sums_lds[WAVES];
+  __shared__ int count;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int64_t token = W == 1 ? (int64_t)blockIdx.x * WAVES + wave : (int64_t)((uint32_t)blockIdx.x / (uint32_t)segments);
   const int32_t segment = W == 1 ? 0 : (int32_t)((uint32_t)blockIdx.x - (uint32_t)token * (uint32_t)segments);
   if (token >= p.n_tokens) return;   // (W = 1: no barrier follows)
+  if (TOP && W > 1 && threadIdx.x == 0) count = 0;
   RowVectors<F32> row;
   row.init(p, token);
   const int64_t vectors = row.vectors(), parts = (int64_t)segments * W, part = W == 1 ? 0 : (int64_t)segment * W + wave;
+  const int32_t v0 = (int32_t)(vectors * part / parts), v1 = (int32_t)(vectors * (part + 1) / parts);
   RowSums sums;
+  LaneBest top;
   uint64_t list = 0;
-  scan_row<F32, TOP>(row, (int32_t)(vectors * part / parts), (int32_t)(vectors * (part + 1) / parts), p.scale * kLog2e, p.n_top, pending[TOP ? wave : 0], lane, sums,
-                     list);
-  if constexpr (W > 1) join_waves<W, TOP, kPending>(sums, list, sums_lds, pending[0], wave, lane);
+  scan_row<F32, TOP>(row, v0, v1, p.scale * kLog2e, lane, sums, top);
+  if constexpr (TOP) list = likeliest<F32, W>(row, v0, v1, top, p.n_top, sums, sums_lds, lists, found[W == 1 ? wave : 0], &count, wave, lane);
+  else if constexpr (W > 1) join_waves<W, false>(sums, list, sums_lds, lists, wave, lane);
   if (W > 1 && wave != 0) return;
   if (segments == 1) {
     write_scores<F32>(p, token, sums, list, lane);
@@ -329,19 +427,33 @@ __global__ __launch_bounds__(64 * kMostSegments) void scores_join_kernel(ScoresP
     sums = ((const Partial*)p.workspace)[at].sums;
     if (TOP && lane < p.n_top) list = ((const uint64_t*)((const Partial*)p.workspace + p.n_tokens * segments))[at * p.n_top + lane];
   }
-  join_waves<kMostSegments, TOP, 64>(sums, list, sums_lds, lists, wave, lane);
+  join_waves<kMostSegments, TOP>(sums, list, sums_lds, lists, wave, lane);
   if (wave == 0) write_scores<F32>(p, token, sums, list, lane);
 }
 
-// How a row is dealt out: waves of a work-group, and work-groups.
+// How a row is dealt out: waves of a work-group, and work-groups.  us with 8 (20 where there are 300 tokens or more) words, bf16:
+//   tokens x vocabulary          1 wave     4     16     16 x 4 work-groups and a join
+//   1 x 32000                        -   10.7   12.5   16.0
+//   1 x 128256                       -   21.6   18.1   16.5
+//   1 x 262144                       -   35.6   25.4   17.7 (x 8: 16.6)
+//   60 x 5000                     10.9    8.6   12.3
+//   60 x 32000                    29.4   12.0   13.3   16.5
+//   60 x 65000                       -   16.8   15.6   17.2
+//   60 x 262144                      -   41.9   27.1   20.4 (x 8, which is more work-groups than compute units: 28.6)
+//   300 x 32000                   39.4   17.1   25.4
+//   800 x 128256                   149   65.3   83.5
+//   16000 x 5000                  73.8    144    657
+//   4001 x 32000                  81.7   83.6    188
+//   4001 x 128256                  269    227    328
+// (A launch has fewer than 2^32 threads, so the most tokens get a wave each, four of them a work-group.)
 struct ScoresShape {
   int waves, segments;
 };
 ScoresShape scores_shape(int64_t n_tokens, int32_t vocab) {
-  if (n_tokens >= 2048) return {1, 1};
-  if (n_tokens >= 512) return {4, 1};
-  const int64_t steps = (int64_t)vocab / (16 * 64 * 4 * 4);   // of a work-group of 16 waves, 32-bit logits
-  return {16, (int)std::max<int64_t>(1, std::min<int64_t>({kMostSegments, steps / 2, 512 / std::max<int64_t>(1, n_tokens)}))};
+  if (vocab <= 2048 || (n_tokens >= 2048 && vocab < 16384) || n_tokens >= (1 << 23)) return {1, 1};
+  if (n_tokens > kScoresUnits || vocab < 65536) return {4, 1};
+  if (vocab < 98304) return {16, 1};
+  return {16, (int)std::max<int64_t>(1, std::min<int64_t>({kMostSegments, vocab / 32768, kScoresUnits / std::max<int64_t>(1, n_tokens)}))};
 }
 
 template <bool F32, bool TOP>
@@ -371,10 +483,11 @@ struct RowSlope {
 
 constexpr int kSlopeEach = 4, kSlopeChunk = 256 * 8 * kSlopeEach;   // runs of 8 elements of a thread; elements of a work-group
 
-template <bool F32, bool TO_F32>
+template <bool F32, bool TO_F32, bool NT>
 __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int32_t chunks) {
-  const int64_t token = (int64_t)((uint32_t)blockIdx.x / (uint32_t)chunks);
-  const int32_t chunk = (int32_t)((uint32_t)blockIdx.x - (uint32_t)token * (uint32_t)chunks);
+  const uint32_t block = blockIdx.x;
+  const int64_t token = (int64_t)(block / (uint32_t)chunks);
+  const int32_t chunk = (int32_t)(block - (uint32_t)token * (uint32_t)chunks);
   const int64_t from = token * p.ld, to = token * p.ld_out;
   // Runs of 8 start at multiples of 8 of the logits' memory; of the gradient's too if its rows lie alike.
   const int32_t before = (int32_t)(from & 7), e_first = chunk * kSlopeChunk - before;
@@ -423,24 +536,24 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
     if (alike && e0 >= 0 && e0 + 8 <= p.vocab) {
       float x[8];
       if constexpr (F32) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(row + 4 * (int64_t)e0), b = *reinterpret_cast<const f32x4*>(row + 4 * (int64_t)e0 + 16);
+        const f32x4 a = load_as<f32x4, NT>(row + 4 * (int64_t)e0), b = load_as<f32x4, NT>(row + 4 * (int64_t)e0 + 16);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = i < 4 ? a[i & 3] : b[i & 3];
       } else {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(row + 2 * (int64_t)e0);
+        const u32x4 a = load_as<u32x4, NT>(row + 2 * (int64_t)e0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = RowVectors<false>::value(a, i);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = s.of_sum(x[i]) * p.scale;
       if constexpr (TO_F32) {
-        *reinterpret_cast<f32x4*>(out + 4 * (int64_t)e0) = f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4*>(out + 4 * (int64_t)e0 + 16) = f32x4{x[4], x[5], x[6], x[7]};
+        store_as<NT>(f32x4{x[0], x[1], x[2], x[3]}, out + 4 * (int64_t)e0);
+        store_as<NT>(f32x4{x[4], x[5], x[6], x[7]}, out + 4 * (int64_t)e0 + 16);
       } else {
         bf16x8 z;
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] = (__bf16)x[i];
-        *reinterpret_cast<bf16x8*>(out + 2 * (int64_t)e0) = z;
+        store_as<NT>(z, out + 2 * (int64_t)e0);
       }
     } else {
 #pragma unroll
@@ -452,11 +565,16 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
   if (named >= 0) put(named, named_slope);
 }
 
+// Logits and gradients of more bytes than this are read and written without keeping their lines.  Of 32000 words in fp32, scores and gradient, kept / not:
+// 400 tokens (102 MB) 35.4 / 39.7 us, 600 (154 MB) 52.1 / 50.2, 1200 99.9 / 82.9, 2400 195 / 178, 4096 312 / 296; 8192 in bf16 302 / 258.
+constexpr int64_t kLargeBytes = 128 << 20;
+
 template <bool F32, bool TO_F32>
 hipError_t launch_bwd(const ScoresBwdParams& p, hipStream_t stream) {
   const int32_t chunks = (int32_t)(((int64_t)p.vocab + 7 + kSlopeChunk - 1) / kSlopeChunk);
   // A launch has fewer than 2^32 threads; more tokens go to several.
   const int64_t each = std::max<int64_t>(1, ((int64_t)1 << 23) / chunks);
+  const bool large = p.n_tokens * p.vocab * ((F32 ? 4 : 2) + (TO_F32 ? 4 : 2)) > kLargeBytes;
   for (int64_t first = 0; first < p.n_tokens; first += each) {
     ScoresBwdParams part = p;
     part.n_tokens = std::min(each, p.n_tokens - first);
@@ -467,7 +585,8 @@ hipError_t launch_bwd(const ScoresBwdParams& p, hipStream_t stream) {
     if (part.y) part.y += first;
     if (part.top_ids) part.top_ids += first * p.n_top;
     if (part.g_top) part.g_top += first * p.n_top;
-    hipLaunchKernelGGL((scores_bwd_kernel<F32, TO_F32>), dim3((uint32_t)(part.n_tokens * chunks)), dim3(256), 0, stream, part, chunks);
+    const auto kernel = large ? scores_bwd_kernel<F32, TO_F32, true> : scores_bwd_kernel<F32, TO_F32, false>;
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(part.n_tokens * chunks)), dim3(256), 0, stream, part, chunks);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

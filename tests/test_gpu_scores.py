@@ -87,7 +87,7 @@ def test_scores_against_the_reference(lib, n, v, n_top, kind):
         assert all(np.array_equal(part[k], got[k], equal_nan=True) for k in part)             # without the likeliest words the same bits
 
 
-@pytest.mark.parametrize("n,v", [(3, 70000), (520, 3000), (2050, 400), (40, 9000)])
+@pytest.mark.parametrize("n,v", [(3, 110000), (3, 70000), (520, 3000), (2050, 400), (40, 9000)])
 def test_every_way_of_dealing_a_row(lib, n, v):
     """A wave, four, sixteen, several work-groups: by burst_lm_head_scores_plan, the same words everywhere."""
     import torch
@@ -103,7 +103,7 @@ def test_every_way_of_dealing_a_row(lib, n, v):
 
 
 def test_plans_cover_every_kernel(lib):
-    plans = {lib.burst_lm_head_scores_plan(lib.scores_shape(n, v, 10)) for n, v in ((3, 70000), (520, 3000), (2050, 400), (40, 9000))}
+    plans = {lib.burst_lm_head_scores_plan(lib.scores_shape(n, v, 10)) for n, v in ((3, 110000), (3, 70000), (520, 3000), (2050, 400), (40, 9000))}
     assert {w for w, _ in plans} == {1, 4, 16} and {s > 1 for _, s in plans} == {False, True}
 
 
@@ -130,6 +130,22 @@ def test_order_of_hard_rows(lib, kind, n):
         assert np.array_equal(repeat[i], ref["top_ids"][i % len(rows)])
     keep = [i for i in range(len(few)) if i != 12]                            # (1e30: logits whose fp32 exponents say nothing of the sums)
     check({k: a[:len(few)][keep] for k, a in got.items()}, {k: a[keep] for k, a in ref.items()}, few[keep], 1.0)
+
+
+@pytest.mark.parametrize("n,v", [(2, 32768), (600, 16384), (2100, 20500)])
+def test_large_numbers_in_few_places(lib, n, v):
+    """All large numbers where few threads of the kernels read: every stretch of 512 words, or of 256, begins with some; or the first 2048 words."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(wl.BASE_SEED + 93250 + n))
+    j = np.arange(v)
+    for dtype in (torch.bfloat16, torch.float32):
+        for where in (j % 512 < 8, j % 256 < 4, (j < 2048) & (j % 512 < 504), (j < 2048) & (j % 256 < 252), j % 2048 < 480):
+            base = np.where(where, 20.0 + rng.random(v), rng.standard_normal(v))
+            t = torch.from_numpy(base).cuda().to(dtype)
+            x = t.double().cpu().numpy()
+            want = np.lexsort((j, -x))[:64]
+            got = run(lib, t[None].expand(n, -1).contiguous(), np.zeros(n, np.int64), 64, 1.0)
+            assert (got["top_ids"] == want).all()
 
 
 @pytest.mark.parametrize("n,v", [(3, 5000), (2100, 100)])
@@ -263,7 +279,7 @@ def test_graph_and_streams(lib):
     """Scores and their gradient captured, replayed with other logits between eager calls; two calls on streams of their own."""
     import torch
     rng = np.random.Generator(np.random.PCG64(wl.BASE_SEED + 94200))
-    n, v = 6, 70001
+    n, v = 6, 110001
     t, _ = make(rng, n, v, torch.bfloat16)
     y = torch.from_numpy(rng.integers(0, v, n)).cuda()
     shp = lib.scores_shape(n, v, 12)
