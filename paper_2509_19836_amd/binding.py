@@ -25,6 +25,7 @@ BURST_BF16, BURST_F32, BURST_F8E4M3 = 0, 1, 2
 BURST_MASK_FULL, BURST_MASK_CAUSAL = 0, 1
 BURST_ACC_DQ, BURST_ACC_DK, BURST_ACC_DV = 1, 2, 4
 BURST_MAX_STEPS = 1024
+BURST_TREE_MAX_TOKENS, BURST_CACHE_MAX_LAYERS, BURST_SCORES_MAX_TOP = 64, 1024, 64
 BURST_KERNEL_DQ, BURST_KERNEL_DKDV, BURST_KERNEL_DEALT, BURST_KERNEL_SHARED_CU, BURST_KERNEL_KEY_TILES_64 = 1, 2, 4, 8, 16
 
 
