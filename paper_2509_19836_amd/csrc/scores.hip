@@ -38,21 +38,6 @@ __device__ __forceinline__ float number_of(uint64_t entry) {
 }
 __device__ __forceinline__ bool is_nan(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7fffffffu) > 0x7f800000u; }
 
-// The value of the lane that differs by STEP.  By the vector unit's own moves, not through LDS: a stage of the networks below in a quarter of the time.
-template <int STEP>
-__device__ __forceinline__ uint32_t of_lane_xor(uint32_t x) {
-  if constexpr (STEP == 1) return __builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, false);         // quad_perm [1, 0, 3, 2]
-  else if constexpr (STEP == 2) return __builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, false);    // quad_perm [2, 3, 0, 1]
-  else if constexpr (STEP == 4) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, false), 0x1b, 0xf, 0xf, false);   // 8 lanes, then 4, the other way round
-  else if constexpr (STEP == 8) return __builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, false);   // row_ror 8
-  else if constexpr (STEP == 16) {
-    const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    return (threadIdx.x & 16) ? y[0] : y[1];
-  } else {
-    const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return (threadIdx.x & 32) ? y[0] : y[1];
-  }
-}
 // One stage of a bitonic network over the lanes: of the two lanes that STEP parts, the one below keeps the larger if `larger_below`.
 template <int STEP>
 __device__ __forceinline__ uint64_t exchanged(uint64_t x, bool larger_below, int lane) {
@@ -481,13 +466,15 @@ struct RowSlope {
   }
 };
 
-constexpr int kSlopeEach = 4, kSlopeChunk = 256 * 8 * kSlopeEach;   // runs of 8 elements of a thread; elements of a work-group
+constexpr int kSlopeChunk = 8192;   // elements of a part of a row
 
-template <bool F32, bool TO_F32, bool NT>
+// T: threads of a part, of which a work-group of 256 has one or four.
+template <bool F32, bool TO_F32, bool NT, int T>
 __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int32_t chunks) {
-  const uint32_t block = blockIdx.x;
-  const int64_t token = (int64_t)(block / (uint32_t)chunks);
-  const int32_t chunk = (int32_t)(block - (uint32_t)token * (uint32_t)chunks);
+  const int tid = T == 256 ? (int)threadIdx.x : (int)threadIdx.x & 63;
+  const uint32_t part = T == 256 ? blockIdx.x : blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int64_t number = (int64_t)(part / (uint32_t)chunks), token = number < p.n_tokens ? number : p.n_tokens - 1;   // (the last work-group may have too many parts)
+  const int32_t chunk = (int32_t)(part - (uint32_t)number * (uint32_t)chunks), vocab = number < p.n_tokens ? p.vocab : 0;
   const int64_t from = token * p.ld, to = token * p.ld_out;
   // Runs of 8 start at multiples of 8 of the logits' memory; of the gradient's too if its rows lie alike.
   const int32_t before = (int32_t)(from & 7), e_first = chunk * kSlopeChunk - before;
@@ -502,7 +489,7 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
   s.scale = p.scale;
   const float g_logp = has_y ? p.g_logp[token] : 0.f;
   auto top_id = [&](int k) { return p.top_ids[token * p.n_top + k]; };
-  auto is_word = [&](int64_t id) { return id >= 0 && id < p.vocab; };
+  auto is_word = [&](int64_t id) { return id >= 0 && id < vocab; };
   const int n_top = p.g_top ? p.n_top : 0;
   float g_all = (p.g_lse ? p.g_lse[token] : 0.f) - g_logp;
   for (int k = 0; k < n_top; ++k) g_all -= is_word(top_id(k)) ? p.g_top[token * p.n_top + k] : 0.f;
@@ -515,25 +502,24 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
     else ((__bf16*)out)[i] = (__bf16)x;
   };
 
-  // The word that this thread has to write by itself, if it lies in this part of the row: 0 is the given one, the others the likeliest
-  const int mine = (int)threadIdx.x;
-  int64_t named = -1;
-  if (mine == 0 && has_y) named = y;
-  if (mine >= 1 && mine <= n_top) named = top_id(mine - 1);
-  if (!is_word(named) || named < e_first || named >= e_first + kSlopeChunk) named = -1;
-  float named_slope = 0.f;
-  if (named >= 0) {
-    float g = named == y ? g_logp : 0.f;
-    for (int k = 0; k < n_top; ++k) g += top_id(k) == named ? p.g_top[token * p.n_top + k] : 0.f;
-    named_slope = s.none ? 0.f : (s.of_sum(element(named)) + g) * p.scale;
+  // The words that this thread has to write by itself, if they lie in this part of the row: the given one (thread 0), one of the likeliest
+  int64_t named[2] = {tid == 0 && has_y ? y : -1, tid < n_top ? top_id(tid) : -1};
+  float named_slope[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (!is_word(named[i]) || named[i] < e_first || named[i] >= e_first + kSlopeChunk) named[i] = -1;
+    if (named[i] < 0) continue;
+    float g = has_y && named[i] == y ? g_logp : 0.f;
+    for (int k = 0; k < n_top; ++k) g += top_id(k) == named[i] ? p.g_top[token * p.n_top + k] : 0.f;
+    named_slope[i] = s.none ? 0.f : (s.of_sum(element(named[i])) + g) * p.scale;
   }
   __syncthreads();
 
-#pragma unroll
-  for (int r = 0; r < kSlopeEach; ++r) {
-    const int32_t e0 = e_first + ((int)threadIdx.x + 256 * r) * 8;
-    if (e0 >= p.vocab) continue;
-    if (alike && e0 >= 0 && e0 + 8 <= p.vocab) {
+#pragma unroll 4
+  for (int r = 0; r < kSlopeChunk / (8 * T); ++r) {
+    const int32_t e0 = e_first + (tid + T * r) * 8;
+    if (e0 >= vocab) break;
+    if (alike && e0 >= 0 && e0 + 8 <= vocab) {
       float x[8];
       if constexpr (F32) {
         const f32x4 a = load_as<f32x4, NT>(row + 4 * (int64_t)e0), b = load_as<f32x4, NT>(row + 4 * (int64_t)e0 + 16);
@@ -558,11 +544,13 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (e0 + i >= 0 && e0 + i < p.vocab) put(e0 + i, s.of_sum(element(e0 + i)) * p.scale);
+        if (e0 + i >= 0 && e0 + i < vocab) put(e0 + i, s.of_sum(element(e0 + i)) * p.scale);
     }
   }
   __syncthreads();
-  if (named >= 0) put(named, named_slope);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (named[i] >= 0) put(named[i], named_slope[i]);
 }
 
 // Logits and gradients of more bytes than this are read and written without keeping their lines.  Of 32000 words in fp32, scores and gradient, kept / not:
@@ -574,6 +562,9 @@ hipError_t launch_bwd(const ScoresBwdParams& p, hipStream_t stream) {
   const int32_t chunks = (int32_t)(((int64_t)p.vocab + 7 + kSlopeChunk - 1) / kSlopeChunk);
   // A launch has fewer than 2^32 threads; more tokens go to several.
   const int64_t each = std::max<int64_t>(1, ((int64_t)1 << 23) / chunks);
+  // A wave for a row of few words (scores and gradient in us, bf16, a wave / four: 6107 x 357 16.3 / 24.6, 10211 x 1800 29.9 / 34.6, 10211 x 4154 67.7 / 75.4; in fp32 10211 x
+  // 8000 228 / 208, 300 x 8000 18.6 / 15.3)
+  const bool few = p.vocab <= 4608;
   const bool large = p.n_tokens * p.vocab * ((F32 ? 4 : 2) + (TO_F32 ? 4 : 2)) > kLargeBytes;
   for (int64_t first = 0; first < p.n_tokens; first += each) {
     ScoresBwdParams part = p;
@@ -585,8 +576,10 @@ hipError_t launch_bwd(const ScoresBwdParams& p, hipStream_t stream) {
     if (part.y) part.y += first;
     if (part.top_ids) part.top_ids += first * p.n_top;
     if (part.g_top) part.g_top += first * p.n_top;
-    const auto kernel = large ? scores_bwd_kernel<F32, TO_F32, true> : scores_bwd_kernel<F32, TO_F32, false>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(part.n_tokens * chunks)), dim3(256), 0, stream, part, chunks);
+    const int64_t parts = part.n_tokens * chunks;
+    if (few) hipLaunchKernelGGL((scores_bwd_kernel<F32, TO_F32, false, 64>), dim3((uint32_t)((parts + 3) / 4)), dim3(256), 0, stream, part, chunks);
+    else if (large) hipLaunchKernelGGL((scores_bwd_kernel<F32, TO_F32, true, 256>), dim3((uint32_t)parts), dim3(256), 0, stream, part, chunks);
+    else hipLaunchKernelGGL((scores_bwd_kernel<F32, TO_F32, false, 256>), dim3((uint32_t)parts), dim3(256), 0, stream, part, chunks);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

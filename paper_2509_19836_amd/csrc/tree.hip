@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
         }
       }
     }
-  } while (walk.next(args_here(), direct != 0));
+  } while (walk.next(args_here(), direct != 0, lane));
 }
 
 // A (sequence, new token, query head) whose rows several work-groups had: their pieces added up, in a fixed order.  GROUPS times D / 4 threads take every
@@ -234,7 +234,6 @@ __global__ __launch_bounds__(GROUPS == 1 ? 256 : GROUPS * D / 4) void tree_join_
 }
 
 // How a call is dealt.
-constexpr int kTreeFit = 512;      // work-groups that the chip holds at once, two a CU
 struct TreeShape {
   int32_t columns, blocks, shares;   // columns of a work-group; blocks of them of a key head; shares of the units
   bool direct;                       // a share for every sequence, no workspace
@@ -247,7 +246,10 @@ TreeShape tree_shape(int32_t batch, int32_t sq, int32_t q_heads, int32_t kv_head
   s.columns = all <= 16 ? 16 : all <= 32 ? 32 : all <= 64 ? 64 : 128;
   s.blocks = (all + s.columns - 1) / s.columns;
   const int64_t per_seq = (int64_t)kv_heads * s.blocks, unit = s.columns <= 32 ? 128 : 64, max_units = std::max<int64_t>(1, (max_rows + unit - 1) / unit);
-  s.direct = batch * per_seq >= kTreeFit || max_rows * head_dim <= (s.columns <= 32 ? 512 * 128 : 128 * 128);
+  // A work-group for a whole sequence where they fill the chip, or where its tiles take less time than a second launch: 64 rows with 64 or 128 columns 1.2 us, the
+  // join 4 (us, 64 query heads over 8, 13 tokens, 3 sequences of 128, 256, 512 rows: 10.5, 13.7, 20.1 whole; 14.0, 13.6, 14.6 dealt; 8 heads, 50 tokens, e4m3, 2 of
+  // 256, 512: 12.0, 16.8 and 14.1, 15.2); eight waves with up to 32 columns have 512 rows in two tiles each.
+  s.direct = batch * per_seq >= kTreeFit || (s.columns <= 32 ? max_rows * head_dim <= 512 * 128 : max_rows <= 256);
   s.shares = (int32_t)(s.direct ? batch : std::min<int64_t>(batch * max_units, std::max<int64_t>(1, kTreeFit / per_seq)));
   const int64_t pieces = s.shares * per_seq * 2 * s.columns;
   s.off_ml = up256((int64_t)batch * 8);

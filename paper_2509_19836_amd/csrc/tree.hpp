@@ -46,8 +46,9 @@ struct TreeSeq {
     for (int32_t* x : {&tokens, &hi, &older, &lo, &sinks, &ts, &tf, &units}) *x = __builtin_amdgcn_readfirstlane(*x);
   }
 };
-template <int UNIT>
-__device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int32_t b) {
+// ALIKE: all lanes ask for the same sequence, and look at a token each.
+template <int UNIT, bool ALIKE>
+__device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int32_t b, int lane) {
   TreeSeq s;
   const int32_t n = p.tokens ? p.tokens[b] : p.sq, rows = p.cache.rows_of(b);
   s.tokens = n < 0 ? 0 : n > p.sq ? p.sq : n;
@@ -56,10 +57,31 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int32_t b) {
   const int32_t old = s.older > 0 ? s.older : 0;
   int32_t lo = 0;
   if (p.first) {
-    lo = old;
-    for (int32_t i = 0; i < s.tokens; ++i) {
-      const int32_t f = p.first[b * p.first_sb + i];
-      lo = f < lo ? f : lo;
+    const int32_t* const first = p.first + b * p.first_sb;
+    if constexpr (ALIKE) {
+      const int32_t f = lane < p.sq ? first[lane] : 0;   // (asked for with the numbers above: not by s.tokens)
+      lo = lane < s.tokens ? f : old;
+      auto least = [&](auto step) {
+        const int32_t x = (int32_t)of_lane_xor<decltype(step)::value>((uint32_t)lo);
+        lo = x < lo ? x : lo;
+      };
+      least(std::integral_constant<int, 1>());
+      least(std::integral_constant<int, 2>());
+      least(std::integral_constant<int, 4>());
+      least(std::integral_constant<int, 8>());
+      least(std::integral_constant<int, 16>());
+      least(std::integral_constant<int, 32>());
+      lo = lo < old ? lo : old;
+    } else {
+      constexpr int N = 8;   // loads under way
+      lo = old;
+      for (int32_t i = 0; i < s.tokens; i += N) {
+        int32_t f[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] = first[i + k < s.tokens ? i + k : i];
+#pragma unroll
+        for (int k = 0; k < N; ++k) lo = f[k] < lo ? f[k] : lo;
+      }
     }
     lo = lo > 0 ? lo : 0;
   }
@@ -111,7 +133,7 @@ struct TreeWalk {
     left = 1;
     first_piece = true;
     if (direct) {
-      seq = tree_seq<UNIT>(p, b);
+      seq = tree_seq<UNIT, true>(p, b, lane);
       seq.make_uniform();
       return seq.units > 0;
     }
@@ -126,7 +148,7 @@ struct TreeWalk {
     int32_t total = 0;   // (below 2^31, checked on the host)
     TreeSeq mine = {};
     for (int32_t b0 = 0; b0 < p.batch; b0 += 64) {
-      mine = b0 + lane < p.batch ? tree_seq<UNIT>(p, b0 + lane) : TreeSeq{};
+      mine = b0 + lane < p.batch ? tree_seq<UNIT, false>(p, b0 + lane, lane) : TreeSeq{};
       total += __builtin_amdgcn_readlane(upto(mine.units), 63);
     }
     deal.init(total, shares);
@@ -135,7 +157,7 @@ struct TreeWalk {
     if (left == 0) return false;
     int32_t passed = 0;
     for (int32_t b0 = 0;; b0 += 64) {   // (unit < total: one sequence has it)
-      if (p.batch > 64) mine = b0 + lane < p.batch ? tree_seq<UNIT>(p, b0 + lane) : TreeSeq{};
+      if (p.batch > 64) mine = b0 + lane < p.batch ? tree_seq<UNIT, false>(p, b0 + lane, lane) : TreeSeq{};
       const int32_t end = passed + upto(mine.units), begin = end - mine.units;
       const uint64_t has = __ballot(begin <= unit && unit < end);
       if (has != 0) {
@@ -160,14 +182,14 @@ struct TreeWalk {
       ws.owners[b] = int2{share, 2 * last + (first_piece ? 0 : 1)};
     }
   }
-  __device__ __forceinline__ bool next(const TreeParams& p, bool direct) {
+  __device__ __forceinline__ bool next(const TreeParams& p, bool direct, int lane) {
     if (direct) return false;
     first_piece = false;
     unit += take;
     left -= take;
     at = 0;
     if (left <= 0) return false;
-    seq = tree_seq<UNIT>(p, ++b);
+    seq = tree_seq<UNIT, true>(p, ++b, lane);
     seq.make_uniform();
     return true;
   }
@@ -530,5 +552,6 @@ struct TreeRun {
 };
 
 hipError_t launch_tree_few(const TreeParams& p, const TreeSpace& ws, int32_t columns, int32_t shares, bool direct, hipStream_t stream);
+constexpr int kTreeFit = 512;      // work-groups of four waves that the chip holds at once, two a CU
 
 }  // namespace burst

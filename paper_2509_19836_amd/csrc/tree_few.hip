@@ -10,7 +10,7 @@ namespace {
 
 constexpr int few_slots(int head_dim, bool f8) { return (1 << 14) / (2 * 32 * head_dim * (f8 ? 1 : 2)); }   // 16 KiB a wave
 
-// NB: blocks of 16 columns.  NW: waves of a work-group, four where rows are dealt to many, eight where a work-group has a whole sequence.
+// NB: blocks of 16 columns.  NW: waves of a work-group, four where rows are dealt to many.
 template <int D, bool F8, bool PAGES16, int NB, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void tree_few_kernel(TreeParams, TreeSpace ws, int32_t shares, int32_t direct) {
   using Columns = TreeColumns<D, F8, NB, 3, D == 128 && !F8 && !PAGES16 && NB == 2 ? 1 : 4, 1>;   // (registers)
@@ -138,23 +138,38 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_few_kernel(TreeParams, TreeSp
       }
     }
     __syncthreads();
-  } while (walk.next(args_here(), direct != 0));
+  } while (walk.next(args_here(), direct != 0, lane));
 }
 
 template <int D, bool F8, bool PAGES16, int NB, int NW>
-hipError_t launch_kernel(const TreeParams& p, const TreeSpace& ws, int32_t shares, hipStream_t stream) {
+hipError_t launch_kernel(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream) {
   constexpr int LDS = NW * ((1 << 14) + 16 * NB * 8);
-  hipLaunchKernelGGL((tree_few_kernel<D, F8, PAGES16, NB, NW>), dim3((uint32_t)((int64_t)shares * p.kv_heads)), dim3(64 * NW), LDS, stream, p, ws, shares, NW == 8 ? 1 : 0);
+  const int64_t groups = (int64_t)shares * p.kv_heads;
+  hipLaunchKernelGGL((tree_few_kernel<D, F8, PAGES16, NB, NW>), dim3((uint32_t)groups), dim3(64 * NW), LDS, stream, p, ws, shares, direct ? 1 : 0);
   return hipGetLastError();
+}
+template <int D, bool F8, bool PAGES16, int NB>
+hipError_t launch_waves(const TreeParams& p, const TreeSpace& ws, int32_t shares, bool direct, hipStream_t stream) {
+  // Where a work-group has a whole sequence, eight waves if it has tiles for them and a CU to itself, else few enough that its others find room.  us with 1, 2, 4
+  // and 8 waves (bf16, head_dim 128 if not said):
+  //   4 heads x 3 sequences of 30 rows   7.9, 7.5, 7.2, 8.1;   of 120 rows   10.9, 8.4, 7.1, 8.4;   of 500 rows   24.1, 15.0, 10.5, 9.5
+  //   16 x 128 of 31 (e4m3, 31 tokens)   18.7, 30.8, 41.4, 73.6;   8 x 128 of up to 75 (head_dim 64)   12.3, 10.9, 15.1, 26.5
+  //   8 x 64 of up to 200   16.4, 12.8, 11.4, 15.3;   8 x 128 of up to 1000   78.0, 59.7, 56.2, 66.5;   of up to 8000   518, 352, 281, 292
+  const int32_t tiles = (p.max_rows + 31) / 32;
+  const bool many = (int64_t)shares * p.kv_heads >= kTreeFit;
+  if (direct && !many && tiles > 4) return launch_kernel<D, F8, PAGES16, NB, 8>(p, ws, shares, direct, stream);
+  if (direct && many && tiles <= 1) return launch_kernel<D, F8, PAGES16, NB, 1>(p, ws, shares, direct, stream);
+  if (direct && many && tiles <= 4) return launch_kernel<D, F8, PAGES16, NB, 2>(p, ws, shares, direct, stream);
+  return launch_kernel<D, F8, PAGES16, NB, 4>(p, ws, shares, direct, stream);
 }
 template <int D, bool F8, bool PAGES16>
 hipError_t launch(const TreeParams& p, const TreeSpace& ws, int32_t columns, int32_t shares, bool direct, hipStream_t stream) {
-  if (columns == 16) return direct ? launch_kernel<D, F8, PAGES16, 1, 8>(p, ws, shares, stream) : launch_kernel<D, F8, PAGES16, 1, 4>(p, ws, shares, stream);
-  return direct ? launch_kernel<D, F8, PAGES16, 2, 8>(p, ws, shares, stream) : launch_kernel<D, F8, PAGES16, 2, 4>(p, ws, shares, stream);
+  return columns == 16 ? launch_waves<D, F8, PAGES16, 1>(p, ws, shares, direct, stream) : launch_waves<D, F8, PAGES16, 2>(p, ws, shares, direct, stream);
 }
 template <int D, bool F8>
 hipError_t launch(const TreeParams& p, const TreeSpace& ws, int32_t columns, int32_t shares, bool direct, hipStream_t stream) {
-  return p.cache.page_rows % 16 == 0 ? launch<D, F8, true>(p, ws, columns, shares, direct, stream) : launch<D, F8, false>(p, ws, columns, shares, direct, stream);
+  return p.cache.page_rows % 16 == 0 ? launch<D, F8, true>(p, ws, columns, shares, direct, stream)
+                                     : launch<D, F8, false>(p, ws, columns, shares, direct, stream);
 }
 
 }  // namespace
