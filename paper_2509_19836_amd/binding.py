@@ -713,7 +713,9 @@ def cache_layers(caches):
     layers = (burst_cache_t * len(caches))(*caches)
     layers._caches, layers._device = caches, caches[0]._device
     batch, kv_heads, d = caches[0]._sizes
-    layers._shape = burst_shape_t(batch, kv_heads, kv_heads, d, 0, 0, 1.0)
+    # (for 0 .. 64 new rows, made once: a structure takes 0.8 us of a call)
+    layers._shapes = [burst_shape_t(batch, kv_heads, kv_heads, d, sq, 0, 1.0) for sq in range(BURST_TREE_MAX_TOKENS + 2)]
+    layers._per_sequence = (batch,)
     return layers
 
 
@@ -726,7 +728,7 @@ def burst_attn_cache_copy_pages(layers, moves, stream=None):
         _check_device(device, moves)
     if moves.dtype != torch.int32 or moves.dim() != 2 or moves.size(1) != 3 or not moves.is_contiguous():
         raise ValueError("moves: contiguous int32 tensor of [n, 3] expected")
-    _check(_lib.burst_attn_cache_copy_pages(layers._shape, len(layers), layers, moves.data_ptr(), moves.size(0), stream))
+    _check(_lib.burst_attn_cache_copy_pages(layers._shapes[0], len(layers), layers, moves.data_ptr(), moves.size(0), stream))
 
 
 def burst_attn_cache_keep_rows(layers, from_rows, kept, new_rows=None, stream=None):
@@ -736,12 +738,12 @@ def burst_attn_cache_keep_rows(layers, from_rows, kept, new_rows=None, stream=No
         raise _elsewhere(layers, device)
     if from_rows.get_device() != device:
         _check_device(device, from_rows)
-    s = layers._shape
-    if from_rows.dim() != 2 or from_rows.size(0) != s.batch:
-        raise ValueError(f"from_rows: int32 tensor of [{s.batch}, sq] expected")
-    ptr, kept_ptr, new = _int32(from_rows, 2), _numbers(kept, device, s.batch), _numbers(new_rows, device, s.batch)
-    shp = burst_shape_t(s.batch, s.q_heads, s.kv_heads, s.head_dim, from_rows.size(1), 0, 1.0)
-    _check(_lib.burst_attn_cache_keep_rows(shp, len(layers), layers, ptr, from_rows.stride(0) if s.batch > 1 else 0, new, kept_ptr, stream))
+    sizes, stride, n = from_rows.shape, from_rows.stride(), layers._per_sequence
+    if from_rows.dtype is not torch.int32 or len(sizes) != 2 or sizes[0] != n[0] or (sizes[1] > 1 and stride[1] != 1):
+        raise ValueError(f"from_rows: int32 tensor of [{n[0]}, sq] with a contiguous last dimension expected, not {from_rows.dtype} {tuple(sizes)}, strides {stride}")
+    shp = layers._shapes[min(sizes[1], BURST_TREE_MAX_TOKENS + 1)]   # (more are refused)
+    _check(_lib.burst_attn_cache_keep_rows(shp, len(layers), layers, from_rows.data_ptr(), stride[0] if sizes[0] > 1 else 0,
+                                           _per_token(new_rows, torch.int32, n, device), _per_token(kept, torch.int32, n, device), stream))
 
 
 def scores_shape(n_tokens, vocab, n_top=0, scale=1.0):
@@ -776,7 +778,7 @@ def _per_token(t, dtype, sizes, device):
     """The address of a contiguous tensor of these sizes, or None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != sizes or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != sizes or not t.is_contiguous():
         raise ValueError(f"contiguous {dtype} tensor of {sizes} expected, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
     if t.get_device() != device:
         _check_device(device, t)
