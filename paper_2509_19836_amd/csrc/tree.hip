@@ -69,16 +69,19 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
     const bool once = blocks == 1 && direct == 0;   // lines are not kept where rows are many and no other work-group reads them
     typename Run::Pages pages;
     const int32_t end = walk.at + walk.take;
-    uint32_t there[SLOTS];   // of the tiles under way: this wave's rows
-    auto look_up = [&](int32_t u) { run.look_up(walk.row_of(u) + 16 * wave, lane, pages); };
-    auto ask = [&](int32_t u, int slot) {
+    uint32_t there[SLOTS];   // of the tiles under way: this wave's rows; all rows (PAGES16: each wave looks at all pages; else the waves tell each other)
+    uint64_t rows_of[SLOTS];
+    auto look_up = [&](int32_t u) { run.look_up([&](int32_t v) { return walk.row_of(v) + 16 * wave; }, u, walk.at, end, wave, lane, pages); };
+    auto ask = [&](int32_t u, int slot, uint64_t& rows) {
       const int32_t row0 = walk.row_of(u);
+      rows = some.rows(row0);
+      if constexpr (PAGES16) rows &= run.with_page(pages, u);
       typename Run::Place place;
-      run.place(row0 + 16 * wave, (uint32_t)(some.rows(row0) >> (16 * wave)) & 0xffffu, lane, pages, place);
+      run.place(row0 + 16 * wave, (uint32_t)(rows >> (16 * wave)) & 0xffffu, lane, pages, u, 0, place);
       const uint32_t kt = lds0 + slot * 2 * TILE + wave * Run::BYTES;
       run.template bring<false>(place, 0, kt, once);
       run.template bring<true>(place, 0, kt + TILE, once);
-      if (lane == 0) ((lds_u16)there_lds)[slot * 4 + wave] = (uint16_t)place.there;
+      if (!PAGES16 && lane == 0) ((lds_u16)there_lds)[slot * 4 + wave] = (uint16_t)place.there;
       return place.there;
     };
     look_up(walk.at);
@@ -86,7 +89,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
     for (int i = 0; i + 1 < SLOTS; ++i) {
       there[i] = 0xffffu;
       if (walk.at + i < end) {
-        there[i] = ask(walk.at + i, i);
+        there[i] = ask(walk.at + i, i, rows_of[i]);
         if (walk.at + i + 1 < end) look_up(walk.at + i + 1);
       }
     }
@@ -98,11 +101,15 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, Tr
       char* const tile = smem + slot * 2 * TILE;
       Run::clear(tile + TILE + wave * Run::BYTES, there[0], lane);
       lds_barrier();            // the tile is there, and all waves have left the one before
+      uint64_t rows_there = rows_of[0];
+      if constexpr (!PAGES16) rows_there = uniform(((lds_u64)there_lds)[slot]);
 #pragma unroll
-      for (int i = 0; i + 2 < SLOTS; ++i) there[i] = there[i + 1];
-      const uint64_t rows_there = uniform(((lds_u64)there_lds)[slot]);
+      for (int i = 0; i + 2 < SLOTS; ++i) {
+        there[i] = there[i + 1];
+        rows_of[i] = rows_of[i + 1];
+      }
       if (u + SLOTS - 1 < end) {
-        there[SLOTS - 2] = ask(u + SLOTS - 1, next_slot);
+        there[SLOTS - 2] = ask(u + SLOTS - 1, next_slot, rows_of[SLOTS - 2]);
         if (u + SLOTS < end) look_up(u + SLOTS);
       }
       if (live) {

@@ -199,7 +199,7 @@ struct TreeWalk {
 // What some token of a sequence sees of the 64 rows from t0 on.
 struct TreeUnion {
   uint64_t word;
-  int32_t older, lo, sinks, hi;
+  int32_t older, lo, sinks, hi, inside;
   __device__ __forceinline__ void init(const TreeParams& p, const TreeSeq& s, int32_t b, int lane) {
     uint64_t w = 0;
     if (lane < s.tokens && !p.elsewhere) w = (p.seen ? p.seen[b * p.seen_sb + lane] : low_bits(lane + 1)) & low_bits(s.tokens);
@@ -210,8 +210,10 @@ struct TreeUnion {
     lo = s.lo;
     sinks = s.sinks;
     hi = s.hi;
+    inside = s.older < s.hi ? s.older : s.hi;   // rows from lo up to here are all seen
   }
   __device__ __forceinline__ uint64_t rows(int32_t t0) const {
+    if (t0 >= lo && t0 + 64 <= inside) return ~0ull;   // (most tiles: scalar arithmetic is a good part of a tile's time)
     return (rows_between(lo, older, t0) | rows_between(0, sinks, t0) | moved(word, older - t0)) & low_bits(hi - t0);
   }
 };
@@ -447,7 +449,6 @@ __device__ __forceinline__ void load_to_lds_once(const char* base, uint32_t offs
 template <int D, bool F8, bool PAGES16, int HALVES>
 struct TreeRun {
   static constexpr int kBytes = F8 ? 1 : 2, PER_ROW = D * kBytes / 16, RPI = 64 / PER_ROW, NI = 16 / RPI, BYTES = 16 * D * kBytes;
-  typedef const __attribute__((address_space(4))) int32_t* scalar_table;
   const char *k_base, *v_base;
   const int32_t* table;
   int64_t s_page, s_row;
@@ -476,18 +477,56 @@ struct TreeRun {
         if constexpr (PAGES16) off[h][i] = row * (uint32_t)s_row + piece[h][i];
       }
   }
+  // The pages of a run's rows.  PAGES16: of 64 / HALVES tiles at once, a lane for each run, as a scalar load for each tile would make every wait for LDS operands
+  // a wait for that load too (they count in one counter, and it comes back in any order).
+  static constexpr int TILES = PAGES16 ? 64 / HALVES : 1;
   struct Pages {
-    int32_t page[PAGES16 ? 1 : NI];
+    int32_t page[PAGES16 ? 1 : HALVES * NI], from;
+    uint64_t all, each[4];   // PAGES16, HALVES 1: tiles whose four runs have a page, and those of each run
   };
-  __device__ __forceinline__ void look_up(int32_t row0, int lane, Pages& x) const {
-    if constexpr (PAGES16) {
-      x.page[0] = row0 < hi ? ((scalar_table)table)[by_page.quotient(row0)] : -1;
+  // Of the 64 rows of tile u those whose run has a page (PAGES16, HALVES 1)
+  __device__ __forceinline__ uint64_t with_page(const Pages& x, int32_t u) const {
+    const int32_t i = u - x.from;
+    if ((x.all >> i) & 1) return ~0ull;
+    uint64_t rows = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) rows |= ((x.each[k] >> i) & 1) * (0xffffull << (16 * k));
+    return rows;
+  }
+  // Of tile u (first_row(u): this wave's first row of it), if they have not been looked up; tiles come one after the other, the first one is `begin`.  run: this wave's
+  // of the four of a tile (HALVES 1).
+  template <class FirstRow>
+  __device__ __forceinline__ void look_up(FirstRow first_row, int32_t u, int32_t begin, int32_t end, int run, int lane, Pages& x) const {
+    if constexpr (PAGES16 && HALVES == 1) {
+      if (u != begin && u != x.from + TILES) return;
+      const int32_t row0 = first_row(u + lane) - 16 * run;
+      int32_t page[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) page[k] = u + lane < end && row0 + 16 * k < hi ? table[by_page.quotient(row0 + 16 * k)] : -1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(page[k]));   // (waited for here: at its uses the compiler would wait in every tile, for all loads under way)
+      x.all = ~0ull;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x.each[k] = __ballot(page[k] >= 0 && page[k] < n_pages);
+        x.all &= x.each[k];
+      }
+      x.page[0] = run == 0 ? page[0] : run == 1 ? page[1] : run == 2 ? page[2] : page[3];
+      x.from = u;
+    } else if constexpr (PAGES16) {
+      if (u != begin && u != x.from + TILES) return;
+      const int32_t tile = u + lane % TILES, row0 = first_row(tile) + 16 * (lane / TILES);
+      x.page[0] = tile < end && row0 < hi ? table[by_page.quotient(row0)] : -1;
+      asm volatile("" : "+v"(x.page[0]));   // (as above)
+      x.from = u;
     } else {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int32_t row = row0 + row_in(i, lane);
-        x.page[i] = row < hi ? table[by_page.quotient(row)] : -1;
-      }
+      for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int32_t row = first_row(u) + 16 * h + row_in(i, lane);
+          x.page[h * NI + i] = row < hi ? table[by_page.quotient(row)] : -1;
+        }
     }
   }
   // Where the run lies, and which of its rows are brought (bits, the same in all lanes)
@@ -495,9 +534,10 @@ struct TreeRun {
     uint32_t there;
     int64_t at[PAGES16 ? 1 : NI];   // bytes, of the run's first row or of this lane's rows
   };
-  __device__ __forceinline__ void place(int32_t row0, uint32_t rows, int lane, const Pages& x, Place& to) const {
+  // row0: first row of run h of tile u
+  __device__ __forceinline__ void place(int32_t row0, uint32_t rows, int lane, const Pages& x, int32_t u, int h, Place& to) const {
     if constexpr (PAGES16) {
-      const int32_t page = x.page[0], in_page = row0 - by_page.quotient(row0) * page_rows;
+      const int32_t page = __builtin_amdgcn_readlane(x.page[0], u - x.from + TILES * h), in_page = row0 - by_page.quotient(row0) * page_rows;
       to.there = page >= 0 && page < n_pages ? rows : 0u;
       to.at[0] = to.there ? page * s_page + in_page * s_row : 0;
     } else {
@@ -506,8 +546,8 @@ struct TreeRun {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int32_t row = row0 + row_in(i, lane), in_page = row - by_page.quotient(row) * page_rows;
-        const bool there = ((rows >> row_in(i, lane)) & 1) && x.page[i] >= 0 && x.page[i] < n_pages;
-        to.at[i] = there ? x.page[i] * s_page + in_page * s_row : 0;
+        const bool there = ((rows >> row_in(i, lane)) & 1) && x.page[h * NI + i] >= 0 && x.page[h * NI + i] < n_pages;
+        to.at[i] = there ? x.page[h * NI + i] * s_page + in_page * s_row : 0;
         mine |= there ? 1u << i : 0u;
         all = all && there;
       }

@@ -45,19 +45,20 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_few_kernel(TreeParams, TreeSp
     // This wave's tiles: rows of unit u from 32 wave on, two runs of 16.  Tile u + SLOTS takes the place of tile u: its keys are asked for when the scores of u
     // have been formed, its values when the products with P are done.
     const bool once = direct == 0;   // lines are not kept where rows are many
-    typename Run::Pages pages[2];
+    typename Run::Pages pages;
     typename Run::Place place[2];
     const int32_t end = walk.at + walk.take;
     uint32_t there[SLOTS];
     auto first_row = [&](int32_t u) { return walk.row_of(u) + 32 * wave; };
+    constexpr bool EARLY = PAGES16 || F8 || D == 64 || NB == 1;   // (else the pages' numbers find no registers beside the products)
     auto look_up = [&](int32_t u) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) run.look_up(first_row(u) + 16 * h, lane, pages[h]);
+      if (EARLY) run.look_up(first_row, u, walk.at, end, 0, lane, pages);
     };
     auto put = [&](int32_t u) {
+      if (!EARLY) run.look_up(first_row, u, walk.at, end, 0, lane, pages);
       const uint32_t rows = (uint32_t)some.rows(first_row(u));
 #pragma unroll
-      for (int h = 0; h < 2; ++h) run.place(first_row(u) + 16 * h, (rows >> (16 * h)) & 0xffffu, lane, pages[h], place[h]);
+      for (int h = 0; h < 2; ++h) run.place(first_row(u) + 16 * h, (rows >> (16 * h)) & 0xffffu, lane, pages, u, h, place[h]);
       return place[0].there | place[1].there << 16;
     };
     auto ask_k = [&](uint32_t kt) {
