@@ -256,7 +256,7 @@ TreeShape tree_shape(int32_t batch, int32_t sq, int32_t q_heads, int32_t kv_head
   // A work-group for a whole sequence where they fill the chip, or where its tiles take less time than a second launch: 64 rows with 64 or 128 columns 1.2 us, the
   // join 4 (us, 64 query heads over 8, 13 tokens, 3 sequences of 128, 256, 512 rows: 10.5, 13.7, 20.1 whole; 14.0, 13.6, 14.6 dealt; 8 heads, 50 tokens, e4m3, 2 of
   // 256, 512: 12.0, 16.8 and 14.1, 15.2); eight waves with up to 32 columns have 512 rows in two tiles each.
-  s.direct = batch * per_seq >= kTreeFit || (s.columns <= 32 ? max_rows * head_dim <= 512 * 128 : max_rows <= 256);
+  s.direct = batch * per_seq >= kTreeFit || (s.columns <= 32 ? max_rows * head_dim <= 512 * 128 : max_rows <= (batch * per_seq >= kTreeFit / 2 ? 512 : 256));
   s.shares = (int32_t)(s.direct ? batch : std::min<int64_t>(batch * max_units, std::max<int64_t>(1, kTreeFit / per_seq)));
   const int64_t pieces = s.shares * per_seq * 2 * s.columns;
   s.off_ml = up256((int64_t)batch * 8);
