@@ -253,10 +253,14 @@ TreeShape tree_shape(int32_t batch, int32_t sq, int32_t q_heads, int32_t kv_head
   s.columns = all <= 16 ? 16 : all <= 32 ? 32 : all <= 64 ? 64 : 128;
   s.blocks = (all + s.columns - 1) / s.columns;
   const int64_t per_seq = (int64_t)kv_heads * s.blocks, unit = s.columns <= 32 ? 128 : 64, max_units = std::max<int64_t>(1, (max_rows + unit - 1) / unit);
-  // A work-group for a whole sequence where they fill the chip, or where its tiles take less time than a second launch: 64 rows with 64 or 128 columns 1.2 us, the
-  // join 4 (us, 64 query heads over 8, 13 tokens, 3 sequences of 128, 256, 512 rows: 10.5, 13.7, 20.1 whole; 14.0, 13.6, 14.6 dealt; 8 heads, 50 tokens, e4m3, 2 of
-  // 256, 512: 12.0, 16.8 and 14.1, 15.2); eight waves with up to 32 columns have 512 rows in two tiles each.
-  s.direct = batch * per_seq >= kTreeFit || (s.columns <= 32 ? max_rows * head_dim <= 512 * 128 : max_rows <= (batch * per_seq >= kTreeFit / 2 ? 512 : 256));
+  // A work-group for a whole sequence where they fill the chip, or where its tiles take less time than dealing them out, a second launch and the join of pieces: the
+  // more sequences there are, the longer those take.  us, whole / dealt, bf16, head_dim 128:
+  //   80 columns   32 work-groups: 256 rows 13.1 / 16.8, 512 19.2 / 18.8;   64: 512 19.6 / 22.7, 1024 30.9 / 25.4;   128: 512 20.1 / 25.6, 1024 31.4 / 31.8;
+  //                240: 1024 37.7 / 46.6, 2048 61.6 / 71.4, 4096 109 / 113, of up to 1024 rows 31.4 / 29.5, of up to 4096 101 / 44.9
+  //   16 columns   64 work-groups: 512 rows 10.6 / 14.2, 1024 13.4 / 18.5, 4096 47.8 / 32.0;   240: 1024 29.3 / 31.7, of up to 1024 15.5 / 22.9, of up to 4096 50.5 / 35.8
+  //   16 columns   2 work-groups: 1024 rows 12.5 / 12.5;   32 columns, e4m3: 16.2 / 14.3;   16 columns, head_dim 64: 2040 rows 15.0 / 12.0
+  const int64_t groups = batch * per_seq, whole = s.columns <= 32 ? groups >= 64 ? 1024 : 768 : std::max({(int64_t)256, std::min((int64_t)512, 8 * groups), 4 * groups});
+  s.direct = groups >= kTreeFit || max_rows <= whole;
   s.shares = (int32_t)(s.direct ? batch : std::min<int64_t>(batch * max_units, std::max<int64_t>(1, kTreeFit / per_seq)));
   const int64_t pieces = s.shares * per_seq * 2 * s.columns;
   s.off_ml = up256((int64_t)batch * 8);
