@@ -9,6 +9,8 @@
 // is sorted.  An entry is the number, as a whole one of the same order, over the complement of its index: equal numbers go by the lowest index, rows of equal
 // numbers (masked ones) give a bound that few words reach like any other, and any way of dealing the elements out gives the same words.
 //   A row is a wave's where there are many, else several waves' or several work-groups', whose sums and lists are joined.
+//   Measured: 4001 x 128256 bf16, 20 words 226 us (4.5 TB/s, vector unit 78 % busy; without words 182, 5.6 TB/s); 4096 x 32000 fp32 without words 95 us (5.5 TB/s); 60 x 32000, 8 words 12 us,
+// of which the words are 4.5.  Lists that are kept in order while a row is read took 318 us in the first case.
 #include <algorithm>
 #include <type_traits>
 
@@ -457,6 +459,7 @@ hipError_t launch(const ScoresParams& p, hipStream_t stream) {
 // d x_j = scale * [ p_j (g_lse - g_logp - sum g_top - g_entropy (log p_j + entropy)) + g_logp [j = y] + sum over k of g_top,k [j = id_k] ]
 // Every logit is read once and every gradient written once but for the few words that are named: their logits are read before anything is written (the
 // gradient may take the logits' place), and their gradients written once more, whole, behind the others of their part of the row.
+// Bound by memory: 4096 x 32000 fp32 205 us, 1.05 GB at 5.1 TB/s.  (Four runs of a thread loaded before the first is stored: 50 us more in fp32, nothing in bf16.)
 struct RowSlope {
   float lse, entropy, g_all, g_entropy, scale;
   bool none;   // a row all at -inf

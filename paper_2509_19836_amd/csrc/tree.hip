@@ -1,18 +1,25 @@
 // Attention of a few new tokens of every sequence, a chain or a tree of drafts, over its rows in a paged cache.
 //
 // The new tokens times the query heads that share a key head are the columns of two products: S^T = K Q^T and O^T = V^T P^T, so a row of the
-// cache that is read once serves them all.  A work-group of four waves takes 64 or 128 columns; tiles of 64 rows of K and V come into LDS, where
-// their addresses go by the page table row by row, and each wave multiplies them for 32 columns (all 64 rows for 128 columns of the work-group, half
-// of them for 64, whose halves are added up at the end).
+// cache that is read once serves them all.  Up to 32 columns (tree_few.hip) the cache's bytes bound it, more of them (here) the products and the exponentials.
+// A work-group of four waves takes 64 or 128 columns; tiles of 64 rows of K and V come into LDS by direct loads, where their addresses go by the page table, and
+// each wave multiplies them for 32 columns (all 64 rows for 128 columns of the work-group, half of them for 64, whose halves are added up at the end).
 //   Which rows a column sees is a 64-bit word for each tile: older rows from its first one on and the first rows of all, both intervals, and the
 // new tokens' rows by the bits of its word, moved to where they stand in the tile.  A tile of which every column of a wave sees all rows does not
 // look at them.
-//   The running maximum is a whole number (base 2), so that a rescale changes no bit of P and O.  P goes in as bf16 numbers that add up to it: three for O
-// in fp32, whose 24 bits they are, two for O in bf16 (16 bits, far below what the cast rounds).
+//   The running maximum is a whole number (base 2), so that a rescale changes no bit of P and O.  P goes in as the three bf16 numbers that its 24 bits are; with more
+// than 32 columns and O in bf16 rounded to one, as in a step of the ring: its error, at most 2^-8 of each number, averages out below the 2^-8 that the cast of O rounds
+// (64 columns over 16384 rows x 32 sequences: three parts 404 us in bf16 and 315 in e4m3, one 350 and 242).
 //
 // Work is cut into units of a tile and numbered over (sequence, tiles that some of its tokens see): a window leaves the tiles out that lie between the
 // first rows and its own.  The units are dealt evenly to shares, a work-group each for every key head and block of columns; a piece that is
 // a whole sequence is written out, others go to the workspace and tree_join_kernel adds them up in a fixed order.
+//
+// Measured: 4 sequences of 32768 rows, 64 tokens, 64 query heads over 8 (512 columns, bf16) 304-315 us, 870-904 TFLOP/s, matrix pipe 47 % busy.  A tile takes a wave
+// 1024 clocks of MFMAs and about as many of exponentials and sums; scalar work on masks and pages was a third of the rest (looked up tile by tile 324-347 us).
+// Two teams of waves that take these phases in turn, as in a step of the ring, gave nothing here (345-353 us: each team brings tiles of its own), nor did 256 columns a
+// work-group (340).  16 sequences of up to 4096 rows, 12 tokens, 32 over 8 heads: 24 us and a join of 6.5; 32 of up to 49152, a
+// window of 16384, 8 tokens, 64 over 8 heads, e4m3 157 us, 5.0 TB/s.
 #include "tree.hpp"
 
 namespace burst {
@@ -258,8 +265,8 @@ TreeShape tree_shape(int32_t batch, int32_t sq, int32_t q_heads, int32_t kv_head
   //   80 columns   32 work-groups: 256 rows 13.1 / 16.8, 512 19.2 / 18.8;   64: 512 19.6 / 22.7, 1024 30.9 / 25.4;   128: 512 20.1 / 25.6, 1024 31.4 / 31.8;
   //                240: 1024 37.7 / 46.6, 2048 61.6 / 71.4, 4096 109 / 113, of up to 1024 rows 31.4 / 29.5, of up to 4096 101 / 44.9
   //   16 columns   64 work-groups: 512 rows 10.6 / 14.2, 1024 13.4 / 18.5, 4096 47.8 / 32.0;   240: 1024 29.3 / 31.7, of up to 1024 15.5 / 22.9, of up to 4096 50.5 / 35.8
-  //   16 columns   2 work-groups: 1024 rows 12.5 / 12.5;   32 columns, e4m3: 16.2 / 14.3;   16 columns, head_dim 64: 2040 rows 15.0 / 12.0
-  const int64_t groups = batch * per_seq, whole = s.columns <= 32 ? groups >= 64 ? 1024 : 768 : std::max({(int64_t)256, std::min((int64_t)512, 8 * groups), 4 * groups});
+  //   16 columns   2 work-groups: 1024 rows 12.5 / 12.5;   32 columns, e4m3: 16.2 / 14.3;   16 columns, head_dim 64: 2040 rows 15.0 / 12.0, 12 work-groups of 777 10.4 / 11.0
+  const int64_t groups = batch * per_seq, whole = s.columns <= 32 ? s.columns == 16 || groups >= 64 ? 1024 : 768 : std::max({(int64_t)256, std::min((int64_t)512, 8 * groups), 4 * groups});
   s.direct = groups >= kTreeFit || max_rows <= whole;
   s.shares = (int32_t)(s.direct ? batch : std::min<int64_t>(batch * max_units, std::max<int64_t>(1, kTreeFit / per_seq)));
   const int64_t pieces = s.shares * per_seq * 2 * s.columns;

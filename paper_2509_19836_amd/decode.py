@@ -76,25 +76,24 @@ class PagedCache:
         partly filled one are copied into a page of each one's own, in all layers that go by the table (binding.cache_layers; None: this one alone).
         Raises, and changes nothing, where pages run out."""
         targets = list(targets)
-        if len({source, *targets}) != len(targets) + 1 or any(self.lengths[b] for b in targets):
+        if len({source, *targets}) != len(targets) + 1 or min([source, *targets]) < 0 or any(self.lengths[b] for b in targets):
             raise ValueError("empty sequences expected, each of them once")
         full, over = divmod(self.lengths[source], self.page_rows)
         if over and len(targets) > len(self.free):
             raise RuntimeError(f"{len(targets)} pages asked for, {len(self.free)} are free")
-        shared, moves = self.pages[source][:full], []
+        if over and targets:
+            moves = [[self.pages[source][full], page, over] for page in reversed(self.free[-len(targets):])]
+            lib.burst_attn_cache_copy_pages(self.layers if layers is None else layers, torch.tensor(moves, dtype=torch.int32).to(self.rows.device))
+        shared = self.pages[source][:full]
         for b in targets:
             for page in shared:
                 self.holders[page] += 1
             own = self._take(1) if over else []
-            moves += [[self.pages[source][full], page, over] for page in own]
             self.pages[b], self.lengths[b] = shared + own, self.lengths[source]
             self.table[b] = self.table[source]
             if own:
                 self.table[b, full] = own[0]
             self.rows[b] = self.lengths[b]
-        if moves:
-            moves = torch.tensor(moves, dtype=torch.int32).to(self.rows.device)
-            lib.burst_attn_cache_copy_pages(self.layers if layers is None else layers, moves)
 
     def keep(self, new_rows, kept, layers=None):
         """Of the last new_rows[b] rows of each sequence those stay that kept[b] names (0: the first of them), in its order, and the pages behind them are
@@ -132,6 +131,8 @@ class Draft:
 
     def __init__(self, cache, parents, window=None, sink_rows=0, after=None):
         parents = [list(p) for p in parents]
+        if cache.handle._device != torch.cuda.current_device():
+            raise ValueError(f"the cache is on cuda:{cache.handle._device}, the current device is cuda:{torch.cuda.current_device()}")
         if len(parents) != len(cache.lengths) or any(not -1 <= up < i for p in parents for i, up in enumerate(p)):
             raise ValueError(f"for each token of {len(cache.lengths)} sequences the number of an earlier one or -1 expected")
         self.counts = [len(p) for p in parents]
@@ -149,9 +150,9 @@ class Draft:
                 words = [sum(1 << j for j in range(i + 1) if w >> j & 1 and deep[i] - deep[j] < window) for i, w in enumerate(words)]
             seen.append([w - (1 << 64) if w >> 63 else w for w in words] + [0] * (sq - len(p)))
             depth.append(deep + [0] * (sq - len(p)))
+        places = [[n + i for i in deep] for n, deep in zip(older, depth, strict=True)]
         cache.grow(self.counts)
         device = cache.rows.device
-        places = [[n + i for i in deep] for n, deep in zip(older, depth)]
         first = None if window is None else torch.tensor([[max(0, t - window + 1) for t in row] for row in places], dtype=torch.int32).to(device)
         self.positions = torch.tensor([places], dtype=torch.int32).to(device)
         self.new_rows = torch.tensor(self.counts, dtype=torch.int32).to(device)

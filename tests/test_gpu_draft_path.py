@@ -184,7 +184,7 @@ def test_sequences_that_begin_alike(lib):
                 assert x.equal(torch.cat([old, new[b, :n]]))
     assert len(cache.free) == 2                                               # sequence 2 has gone on into another page
     kept = (list(cache.lengths), [list(p) for p in cache.pages], list(cache.free), list(cache.holders), cache.table.clone())
-    for call, error in ((lambda: cache.fork(0, [1]), ValueError), (lambda: cache.fork(3, [3]), ValueError), (lambda: cache.keep([9, 0, 0, 0], [[0], [], [], []]), ValueError),
+    for call, error in ((lambda: cache.fork(0, [1]), ValueError), (lambda: cache.fork(3, [3]), ValueError), (lambda: cache.fork(3, [-1]), ValueError), (lambda: cache.fork(-1, []), ValueError), (lambda: cache.keep([9, 0, 0, 0], [[0], [], [], []]), ValueError),
                         (lambda: cache.keep([2, 0, 0, 0], [[2], [], [], []]), ValueError), (lambda: cache.keep([2, 0, 0], [[0], [], []]), ValueError),
                         (lambda: cache.keep([0, 0, 0, 6], [[], [], [], [0]]), ValueError), (lambda: decode.Draft(cache, [[0], [], [], []]), ValueError),
                         (lambda: decode.Draft(cache, [[], [], [], []]), ValueError), (lambda: decode.Draft(cache, [[-1] * 60, [], [], []]), ValueError)):
@@ -232,6 +232,9 @@ def test_a_draft_over_a_ring(lib):
     owner, after = 1, [sum(r[b] for r in rows) for b in range(B)]
     with pytest.raises(ValueError, match="window"):
         decode.Draft(caches[owner], parents, window=5, after=after)
+    with pytest.raises(ValueError):
+        decode.Draft(caches[owner], parents, after=after[:1])
+    assert caches[owner].lengths == rows[owner]
     draft = decode.Draft(caches[owner], parents, after=after)
     assert draft.positions.tolist() == [[[45, 46, 46, 47, 47, 48, 45], [56, 57, 58, 59, 60, 56, 56]]]
     n = 7
