@@ -134,8 +134,8 @@ hipError_t launch_cache_keep_rows(const KeepRowsParams& p, hipStream_t stream) {
   if (p.sq == 0) return hipSuccess;
   const PagePieces pieces = pieces_of(p.cache.layers);
   const int32_t per_row = pieces.heads * pieces.per_head, pieces_each = std::min(per_row, 256 * kKeepEach / p.sq);
-  constexpr int32_t kMaxZ = 65535;
-  for (int32_t b0 = 0; b0 < p.batch; b0 += kMaxZ) {
+  constexpr int64_t kMaxZ = 65535;
+  for (int64_t b0 = 0; b0 < p.batch; b0 += kMaxZ) {
     KeepRowsParams part = p;
     part.from += b0 * p.from_sb;
     part.kept += b0;

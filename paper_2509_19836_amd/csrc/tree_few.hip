@@ -158,10 +158,12 @@ hipError_t launch_waves(const TreeParams& p, const TreeSpace& ws, int32_t shares
   //   4 heads x 3 sequences of 30 rows   7.9, 7.5, 7.2, 8.1;   of 120 rows   10.9, 8.4, 7.1, 8.4;   of 500 rows   24.1, 15.0, 10.5, 9.5
   //   16 x 128 of 31 (e4m3, 31 tokens)   18.7, 30.8, 41.4, 73.6;   8 x 128 of up to 75 (head_dim 64)   12.3, 10.9, 15.1, 26.5
   //   8 x 64 of up to 200   16.4, 12.8, 11.4, 15.3;   8 x 128 of up to 1000   78.0, 59.7, 56.2, 66.5;   of up to 8000   518, 352, 281, 292
+  // (A launch has fewer than 2^32 threads: the most sequences get a wave each.)
   const int32_t tiles = (p.max_rows + 31) / 32;
-  const bool many = (int64_t)shares * p.kv_heads >= kTreeFit;
+  const int64_t groups = (int64_t)shares * p.kv_heads;
+  const bool many = groups >= kTreeFit;
   if (direct && !many && tiles > 4) return launch_kernel<D, F8, PAGES16, NB, 8>(p, ws, shares, direct, stream);
-  if (direct && many && tiles <= 1) return launch_kernel<D, F8, PAGES16, NB, 1>(p, ws, shares, direct, stream);
+  if (direct && many && (tiles <= 1 || groups >= 1 << 24)) return launch_kernel<D, F8, PAGES16, NB, 1>(p, ws, shares, direct, stream);
   if (direct && many && tiles <= 4) return launch_kernel<D, F8, PAGES16, NB, 2>(p, ws, shares, direct, stream);
   return launch_kernel<D, F8, PAGES16, NB, 4>(p, ws, shares, direct, stream);
 }

@@ -395,6 +395,27 @@ def test_streams_of_their_own(lib):
         assert torch.equal(o, o2) and torch.equal(l, l2)
 
 
+def test_more_sequences_than_a_launch_has_threads_for(lib):
+    """2^24 sequences and some of more than a tile, which in work-groups of four waves would be 2^32 threads: as many rows, the same result."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(wl.BASE_SEED + 91700))
+    B, d, longest, some = (1 << 24) + 100, 64, 150, 128
+    P = tp.Paged(lib, rng, [longest], 160, 1, d)
+    table = torch.from_numpy(P.table.astype(np.int32)).cuda().expand(B, -1)
+    lengths = torch.arange(B, device="cuda", dtype=torch.int32) % some + (longest - some + 1)
+    cache = lib.paged_cache(P.dev["k"], P.dev["v"], table, lengths)
+    q, q_host = queries(rng, 1, 1, 1, d)
+    shp = lib.shape(B, 1, 1, d, 1, longest, 0.125)
+    assert lib.burst_attn_tree_plan(shp) == (B, 16, True) and lib.burst_attn_tree_workspace_bytes(shp) == 0
+    o = torch.full((B, 1, 1, d), 7.0, device="cuda", dtype=torch.bfloat16)
+    lib.burst_attn_tree(shp, cache, lib.tree(), q.expand(B, -1, -1, -1), o)
+    torch.cuda.synchronize()
+    rows = lengths[:some].tolist()
+    ref = co.tree(np.repeat(q_host, some, 0), P.host["k"], P.host["v"], np.repeat(P.table, some, 0), rows, [1] * some, 0.125)
+    check_tree(o[:some], None, ref, longest, d, bf16=True)
+    assert torch.equal(o[some:].view(torch.int16), o[:-some].view(torch.int16))
+
+
 def test_offsets_beyond_32_bits(lib):
     """Pages 1 GiB and heads 4 GiB from each other."""
     import torch
