@@ -151,9 +151,9 @@ typedef struct {
  * sequence's rows, the new ones among them, at most table_cols * page_rows (INVALID_ARG): rows at and behind it are not seen.  batch * q_heads * sq above 2^25, or
  * batch * sk of about 2^36 and more: UNSUPPORTED.
  * O is exact to fp32 rounding before it is cast: the numbers exp(S - Lse) are multiplied in the three bf16 parts that their 24 bits are.  Where O is bf16 and
- * sq * q_heads / kv_heads is above 32 they are rounded to bf16, as in a step of the ring.  A row that is seen by none of a sequence's tokens, or that has no page, may hold anything, NaN too.  An infinity or NaN in a
+ * sq * q_heads / kv_heads is above 32 they are multiplied in two, which hold them to 2^-16.  A row that is seen by none of a sequence's tokens, or that has no page, may hold anything, NaN too.  An infinity or NaN in a
  * row that one of them sees reaches those that see it, and may reach the sequence's other tokens.  A token's result depends on the other tokens and sequences by
- * roundings in fp32 alone.  o and lse share memory with nothing that the call reads.
+ * roundings in fp32 alone, and where two parts are taken by those of 2^-16 of each number, before O is cast.  o and lse share memory with nothing that the call reads.
  * workspace: burst_attn_tree_workspace_bytes(shape) bytes, 256-byte aligned, contents on entry irrelevant, on return unspecified; calls that share one must be
  * ordered on one stream.  The size depends on batch, sq, the heads, head_dim and sk; it is 0 for some shapes, for which workspace may be NULL.
  */

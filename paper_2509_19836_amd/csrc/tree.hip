@@ -8,18 +8,18 @@
 // new tokens' rows by the bits of its word, moved to where they stand in the tile.  A tile of which every column of a wave sees all rows does not
 // look at them.
 //   The running maximum is a whole number (base 2), so that a rescale changes no bit of P and O.  P goes in as the three bf16 numbers that its 24 bits are; with more
-// than 32 columns and O in bf16 rounded to one, as in a step of the ring: its error, at most 2^-8 of each number, averages out below the 2^-8 that the cast of O rounds
-// (64 columns over 16384 rows x 32 sequences: three parts 404 us in bf16 and 315 in e4m3, one 350 and 242).
+// than 32 columns and O in bf16 as two, which hold it to 2^-16: far below the 2^-8 that the cast of O rounds, so that one token more, which may bring a sequence here from
+// tree_few.hip, changes no result by more than that.  (4 x 32768 rows, 512 columns, head_dim 128: three parts 486 us in bf16 and 460 in e4m3, two 398 and 381; one, which is off by
+// 2^-9 of each number, 298 and 289.)
 //
 // Work is cut into units of a tile and numbered over (sequence, tiles that some of its tokens see): a window leaves the tiles out that lie between the
 // first rows and its own.  The units are dealt evenly to shares, a work-group each for every key head and block of columns; a piece that is
 // a whole sequence is written out, others go to the workspace and tree_join_kernel adds them up in a fixed order.
 //
-// Measured: 4 sequences of 32768 rows, 64 tokens, 64 query heads over 8 (512 columns, bf16) 304-315 us, 870-904 TFLOP/s, matrix pipe 47 % busy.  A tile takes a wave
-// 1024 clocks of MFMAs and about as many of exponentials and sums; scalar work on masks and pages was a third of the rest (looked up tile by tile 324-347 us).
-// Two teams of waves that take these phases in turn, as in a step of the ring, gave nothing here (345-353 us: each team brings tiles of its own), nor did 256 columns a
-// work-group (340).  16 sequences of up to 4096 rows, 12 tokens, 32 over 8 heads: 24 us and a join of 6.5; 32 of up to 49152, a
-// window of 16384, 8 tokens, 64 over 8 heads, e4m3 157 us, 5.0 TB/s.
+// Measured, with the join: 4 sequences of 32768 rows, 64 tokens, 64 query heads over 8 (512 columns, bf16) 396-404 us, three products executed for two at 1030 TFLOP/s.  Scalar work on
+// masks and pages is kept out of the tiles (looked up tile by tile it took 8 % more).  Two teams of waves that take products and exponentials in turn, as in a step of the ring, gave nothing here (each
+// team brings tiles of its own), nor did 256 columns a work-group.  16 sequences of up to 4096 rows, 12 tokens, 32 over 8 heads: 25 us and a join of 6.5; 32 of up to 49152, a
+// window of 16384, 8 tokens, 64 over 8 heads, e4m3 165 us, 4.7 TB/s.
 #include "tree.hpp"
 
 namespace burst {
@@ -33,7 +33,7 @@ constexpr int tree_slots(int head_dim, bool f8) { return (1 << 16) / (2 * kTreeR
 // CW: waves side by side, of 32 columns each; the other way they share a tile's rows.
 template <int D, bool F8, bool PAGES16, int CW, int PARTS>
 __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams, TreeSpace ws, int32_t blocks, int32_t shares, int32_t direct) {
-  constexpr int RW = kTreeWaves / CW, CH = RW == 1 && PARTS == 1 ? 2 : 1, PASSES = 2 / RW / CH;
+  constexpr int RW = kTreeWaves / CW, CH = RW == 1 && PARTS <= 2 ? 2 : 1, PASSES = 2 / RW / CH;
   using Columns = TreeColumns<D, F8, 2, PARTS, D == 128 && !F8 && !PAGES16 ? 2 : 4, CH>;   // (registers)
   using Run = TreeRun<D, F8, PAGES16, 1>;
   using Operands = TreeOperands<D, F8>;
@@ -288,9 +288,9 @@ hipError_t launch_columns(const TreeParams& p, const TreeShape& s, const TreeSpa
 }
 template <int D, bool F8, bool PAGES16>
 hipError_t launch_kernel(const TreeParams& p, const TreeShape& s, const TreeSpace& ws, hipStream_t stream) {
-  // P in bf16 where O is, or in three parts
-  if (s.columns == 64) return p.o.is_f32 ? launch_columns<D, F8, PAGES16, 2, 3>(p, s, ws, stream) : launch_columns<D, F8, PAGES16, 2, 1>(p, s, ws, stream);
-  return p.o.is_f32 ? launch_columns<D, F8, PAGES16, 4, 3>(p, s, ws, stream) : launch_columns<D, F8, PAGES16, 4, 1>(p, s, ws, stream);
+  // P in two parts where O is bf16, else in three
+  if (s.columns == 64) return p.o.is_f32 ? launch_columns<D, F8, PAGES16, 2, 3>(p, s, ws, stream) : launch_columns<D, F8, PAGES16, 2, 2>(p, s, ws, stream);
+  return p.o.is_f32 ? launch_columns<D, F8, PAGES16, 4, 3>(p, s, ws, stream) : launch_columns<D, F8, PAGES16, 4, 2>(p, s, ws, stream);
 }
 // Threads for the pieces of a sequence, of which it has as many as shares if it is the only long one.
 template <int D, int COLS>

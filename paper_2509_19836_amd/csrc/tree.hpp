@@ -27,6 +27,10 @@ __device__ __forceinline__ const TreeParams& args_here() {
   return *(const TreeParams*)p;
 }
 
+// The leading 16 bits of two numbers.
+__device__ __forceinline__ u16x2 upper_halves(float x0, float x1) {
+  return __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x1), __builtin_bit_cast(uint32_t, x0), 0x07060302u));
+}
 // The lowest n bits, n of any size.
 __device__ __forceinline__ uint64_t low_bits(int32_t n) { return n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0ull; }
 // Of the 64 rows from t0 on those that are rows lo .. hi - 1.
@@ -275,7 +279,7 @@ struct TreeOperands {
 
 // 16 NB columns of a wave: column 16 nb + r of them is lane r's (and r + 16's, ..).  A column is a token and a query head; what it sees, its query,
 // its running maximum (base 2, a whole number, so that a rescale changes no bit of P and O) and sums.
-// PARTS: bf16 numbers that a P is multiplied in; AHEAD: operands fetched before they are used; CH: 32 rows at a time, or twice as many.
+// PARTS: bf16 numbers that a P is multiplied in, three (all of its 24 bits) or two; AHEAD: operands fetched before they are used; CH: 32 rows at a time, or twice as many.
 template <int D, bool F8, int NB, int PARTS, int AHEAD, int CH>
 struct TreeColumns {
   static constexpr int MB = 2 * CH, DK = D / 32, DB = D / 16, HALF = TreeOperands<D, F8>::TILE;
@@ -363,28 +367,27 @@ struct TreeColumns {
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_exp2f(fmaf(y[e], to_log2, -base));
         l[nb] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
-        if constexpr (PARTS == 1) part[c][nb][0] = pack_pair(f32x4{y[0], y[1], y[2], y[3]}, f32x4{y[4], y[5], y[6], y[7]});
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if constexpr (PARTS > 1) {
-        static_assert(PARTS == 1 || CH == 1, "registers");
+        static_assert(PARTS == 2 || PARTS == 3, "parts");
         u16x2 least[4];
 #pragma unroll
         for (int n = 0; n < PARTS; ++n) {
           u32x4 words;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float &x0 = x[2 * i], &x1 = x[2 * i + 1];
-            const uint32_t two = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x1), __builtin_bit_cast(uint32_t, x0), 0x07060302u);
-            u16x2 bits = __builtin_bit_cast(u16x2, two);
+            float &x0 = y[2 * i], &x1 = y[2 * i + 1];
+            // (the last of two parts is rounded, to 2^-16 of P at most and either way; none is negative)
+            u16x2 bits;
+            if constexpr (PARTS == 2) bits = n == 0 ? upper_halves(x0, x1) : __builtin_bit_cast(u16x2, bf16x2{(__bf16)x0, (__bf16)x1});
+            else bits = upper_halves(x0, x1);
             if (!F8 && n == 0) least[i] = __builtin_elementwise_sub_sat(bits, u16x2{kTreeLeastPart, kTreeLeastPart});
             if (!F8 && n != 0) bits = __builtin_elementwise_max(bits, least[i]);
             words[i] = __builtin_bit_cast(uint32_t, bits);
             x0 -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x0) & 0xffff0000u);   // (exact)
             x1 -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x1) & 0xffff0000u);
           }
-          part[0][nb][n] = __builtin_bit_cast(bf16x8, words);
+          part[c][nb][n] = __builtin_bit_cast(bf16x8, words);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);   // (one block of columns after the other: both at once take the registers of twice as many numbers)
     }
