@@ -98,6 +98,8 @@ int burst_lm_head_loss_noalloc(const burst_lm_head_shape_t* shape, const void* h
  *   logits : [n_tokens][ld], BURST_BF16 or BURST_F32, 16-byte aligned, ld >= vocab, any number (rows that are multiples of 16 bytes are read a little faster).
  *   y      : int64 [n_tokens]; a word outside [0, vocab) marks an ignored token: logp 0.  NULL with logp == NULL.
  *   logp, lse, entropy : fp32 [n_tokens], each NULL if not wanted.  top_logp fp32, top_ids int64 : [n_tokens][n_top], each NULL if not wanted.
+ * Exponentials, logp and top_logp are of differences from the row's largest logit: words and whole rows at large finite numbers (-1e10, the type's lowest) have the scores of these formulas;
+ * a lse beyond the largest fp32 number is an infinity.
  * Words at -inf (masked ones) have no share; where all are, lse = logp = top_logp = -inf and entropy = 0.  A NaN or +inf among a token's logits makes its scores NaN; with a NaN
  * its top_ids are words, but no particular ones.
  * workspace: burst_lm_head_scores_workspace_bytes(shape) bytes, 256-byte aligned, or NULL where that is 0; contents on entry irrelevant; calls that share one must be ordered
@@ -120,7 +122,8 @@ int burst_lm_head_scores(const burst_scores_shape_t* shape, const void* logits, 
  * The gradient of the logits from those of the scores (fp32, of the shapes above, each NULL if there is none, not all of them):
  *   d_logits_ij = scale * ( p_ij (g_lse_i - g_logp_i - sum_k g_top_ik - g_entropy_i (log p_ij + entropy_i)) + g_logp_i [j = y_i] + sum_k g_top_ik [j = top_ids_ik] )
  * lse, and entropy with g_entropy, are those that burst_lm_head_scores gave; y comes with g_logp, top_ids with g_top.  A word outside [0, vocab) takes its gradient with it, among
- * top_ids too; one that is named several times gets the sum.  Where lse is -inf the gradient is 0.  d_logits: [n_tokens][ld_d], bf16 or fp32, overwritten
+ * top_ids too; one that is named several times gets the sum.  Where lse is -inf the gradient is 0; where |lse| is above 4096, of which an fp32 number says too little for p, the row's own
+ * sum is formed again (such rows take several times as long).  d_logits: [n_tokens][ld_d], bf16 or fp32, overwritten
  * (words 0 .. vocab - 1 of each row); it may be logits itself (same type and ld), else they share no memory.
  */
 int burst_lm_head_scores_bwd(const burst_scores_shape_t* shape, const void* logits, int32_t logits_dtype, int64_t ld, const int64_t* y, const float* lse,

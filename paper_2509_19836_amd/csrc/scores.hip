@@ -1,8 +1,9 @@
 // Scores of tokens from logits: log probability of given words, log-sum-exp, entropy and the likeliest words; and the gradient of the logits.
 //
-// Every logit is read once.  With x the logits times scale, m their maximum, l = sum exp(x - m) and w = sum exp(x - m) (x - m):
-//     lse = m + log l,   logp = x_y - lse,   entropy = log l - w / l   (in base 2 inside),
-// kept against a running maximum by each lane of its own elements.
+// Every logit is read once.  With x the logits, m their maximum, e = scale (x - m), l = sum exp e and w = sum (exp e) e:
+//     lse = scale m + log l,   logp = e_y - log l,   entropy = log l - w / l   (in base 2 inside),
+// kept against a running maximum by each lane of its own elements.  The difference is taken before the scale: it is 0 at the maximum whatever its size, so rows and forbidden words at
+// large finite numbers (-1e10, the type's lowest) come out as they should.  (From a product of the maximum, e = x scale - fl(m scale) is its rounding, beyond 128 at numbers of 3e9.)
 //   The likeliest words: while the row is read, each lane keeps the largest number of its elements, the step (32 or 16 elements) where it came first, and the
 // largest of the other steps: nine instructions a step.  The n_top-th of the lanes' largest is a bound that n_top words reach, and only those n_top lanes
 // can have others: they read that step again (and, the few whose second largest reaches the bound, the others), and what reaches the bound, about n_top words,
@@ -66,29 +67,32 @@ __device__ __forceinline__ uint64_t sorted(uint64_t x, int lane) {
 // The 64 largest of a list and of entries sorted the other way round
 __device__ __forceinline__ uint64_t joined(uint64_t list, uint64_t up, int lane) { return merged_down(list > up ? list : up, lane); }
 
+// From differences of logits to base-2 exponents (finite for the largest scales too: 0 has to stay 0)
+__device__ __forceinline__ float exponents_of(float scale) { return fminf(scale * kLog2e, 3.4028235e38f); }
+
 // What a part of a row comes to.
 struct RowSums {
-  float m, l, w;   // of base-2 exponents: maximum, sum of exp2(x - m), sum of exp2(x - m) (x - m)
-  __device__ __forceinline__ void join(const RowSums& o) {
+  float m, l, w;   // largest logit; with e = to_log2 (x - m): sum of exp2(e), sum of exp2(e) e
+  __device__ __forceinline__ void join(const RowSums& o, float to_log2) {
     const float top = fmaxf(m, o.m);
-    const float d0 = m == top ? 0.f : fmaxf(m - top, kNothing), d1 = o.m == top ? 0.f : fmaxf(o.m - top, kNothing);
+    const float d0 = m == top ? 0.f : fmaxf((m - top) * to_log2, kNothing), d1 = o.m == top ? 0.f : fmaxf((o.m - top) * to_log2, kNothing);
     const float f0 = __builtin_amdgcn_exp2f(d0), f1 = __builtin_amdgcn_exp2f(d1);
     w = (w + l * d0) * f0 + (o.w + o.l * d1) * f1;
     l = l * f0 + o.l * f1;
     m = top;
   }
   template <int STEP>
-  __device__ __forceinline__ void join_lane_xor() {
+  __device__ __forceinline__ void join_lane_xor(float to_log2) {
     auto other = [](float x) { return __builtin_bit_cast(float, of_lane_xor<STEP>(__builtin_bit_cast(uint32_t, x))); };
-    join(RowSums{other(m), other(l), other(w)});
+    join(RowSums{other(m), other(l), other(w)}, to_log2);
   }
-  __device__ __forceinline__ void join_lanes() {
-    join_lane_xor<1>();
-    join_lane_xor<2>();
-    join_lane_xor<4>();
-    join_lane_xor<8>();
-    join_lane_xor<16>();
-    join_lane_xor<32>();
+  __device__ __forceinline__ void join_lanes(float to_log2) {
+    join_lane_xor<1>(to_log2);
+    join_lane_xor<2>(to_log2);
+    join_lane_xor<4>(to_log2);
+    join_lane_xor<8>(to_log2);
+    join_lane_xor<16>(to_log2);
+    join_lane_xor<32>(to_log2);
   }
 };
 
@@ -98,12 +102,12 @@ struct RowVectors {
   static constexpr int VEC = F32 ? 4 : 8;
   const char* row;      // its first element
   int32_t before, vocab;   // elements of the first vector that lie before it
-  __device__ __forceinline__ void init(const ScoresParams& p, int64_t token) {
-    const int64_t at = token * p.ld;
+  __device__ __forceinline__ void init(const void* logits, int64_t at, int32_t words) {   // at: the row's first element
     before = (int32_t)(at & (VEC - 1));
-    row = (const char*)p.logits + at * (F32 ? 4 : 2);
-    vocab = p.vocab;
+    row = (const char*)logits + at * (F32 ? 4 : 2);
+    vocab = words;
   }
+  __device__ __forceinline__ void init(const ScoresParams& p, int64_t token) { init(p.logits, token * p.ld, p.vocab); }
   __device__ __forceinline__ int32_t vectors() const { return (int32_t)(((int64_t)before + vocab + VEC - 1) / VEC); }
   __device__ __forceinline__ float element(int32_t i) const {
     return F32 ? ((const float*)row)[i] : __builtin_bit_cast(float, (uint32_t)((const uint16_t*)row)[i] << 16);
@@ -170,7 +174,7 @@ __device__ __forceinline__ void scan_row(const RowVectors<F32>& row, int32_t v0,
     const float step = max3(max3(most[0], most[1], most[2]), most[3], -INFINITY);
     if constexpr (TOP) top.see(step, j0);
     // (a scale is positive: the largest logit is the largest exponent)
-    const float m = fmaxf(sums.m, step * to_log2), d = sums.m == m ? 0.f : fmaxf(sums.m - m, kNothing), f = __builtin_amdgcn_exp2f(d);
+    const float m = fmaxf(sums.m, step), d = sums.m == m ? 0.f : fmaxf((sums.m - m) * to_log2, kNothing), f = __builtin_amdgcn_exp2f(d);
     sums.w = (sums.w + sums.l * d) * f;
     sums.l *= f;
     sums.m = m;
@@ -180,7 +184,7 @@ __device__ __forceinline__ void scan_row(const RowVectors<F32>& row, int32_t v0,
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          const float e = fmaf(RowVectors<F32>::value(x[u], i), to_log2, -base), p = __builtin_amdgcn_exp2f(e);
+          const float e = (RowVectors<F32>::value(x[u], i) - base) * to_log2, p = __builtin_amdgcn_exp2f(e);
           sums.l += p;
           sums.w = fmaf(p, decltype(masked_)::value ? fmaxf(e, kNothing) : e, sums.w);
         }
@@ -196,19 +200,19 @@ __device__ __forceinline__ void scan_row(const RowVectors<F32>& row, int32_t v0,
     }
     if (masked) add(std::true_type());
   }
-  sums.join_lanes();
+  sums.join_lanes(to_log2);
 }
 
 // Sums and lists of the work-group's waves, in wave 0.
 template <int W, bool TOP>
-__device__ __forceinline__ void join_waves(RowSums& sums, uint64_t& list, RowSums* sums_lds, uint64_t* lists, int wave, int lane) {
+__device__ __forceinline__ void join_waves(RowSums& sums, uint64_t& list, float to_log2, RowSums* sums_lds, uint64_t* lists, int wave, int lane) {
   if (lane == 0) sums_lds[wave] = sums;
   if (TOP) lists[64 * wave + lane] = list;
   __syncthreads();
 #pragma unroll
   for (int s = 1; s < W; s <<= 1) {
     if (wave % (2 * s) == 0) {
-      sums.join(sums_lds[wave + s]);
+      sums.join(sums_lds[wave + s], to_log2);
       if (lane == 0) sums_lds[wave] = sums;
       if (TOP) {
         list = joined(list, lists[64 * (wave + s) + 63 - lane], lane);
@@ -228,8 +232,8 @@ __device__ __forceinline__ uint64_t of_lane(uint64_t x, int lane) {
 template <int W>
 constexpr int kFound = W == 1 ? 256 : 1024;
 template <bool F32, int W>
-__device__ __forceinline__ uint64_t likeliest(const RowVectors<F32>& row, int32_t v0, int32_t v1, const LaneBest& top, int n_top, RowSums& sums, RowSums* sums_lds,
-                                              uint64_t* lists, uint64_t* found, int* count, int wave, int lane) {
+__device__ __forceinline__ uint64_t likeliest(const RowVectors<F32>& row, int32_t v0, int32_t v1, const LaneBest& top, int n_top, RowSums& sums, float to_log2,
+                                              RowSums* sums_lds, uint64_t* lists, uint64_t* found, int* count, int wave, int lane) {
   constexpr int VEC = RowVectors<F32>::VEC;
   auto index = [&](int32_t j, int i) { return (int32_t)((int64_t)j * VEC - row.before + i); };
   auto is_word = [&](int32_t id, float y) { return (uint32_t)id < (uint32_t)row.vocab && !is_nan(y); };
@@ -251,7 +255,7 @@ __device__ __forceinline__ uint64_t likeliest(const RowVectors<F32>& row, int32_
   if constexpr (W == 1) {
     bound = of_lane(list, n_top - 1);
   } else {
-    join_waves<W, true>(sums, list, sums_lds, lists, wave, lane);
+    join_waves<W, true>(sums, list, to_log2, sums_lds, lists, wave, lane);
     bound = lists[n_top - 1];
   }
   // What reaches it
@@ -344,21 +348,21 @@ __device__ __forceinline__ uint64_t likeliest(const RowVectors<F32>& row, int32_
 template <bool F32>
 __device__ __forceinline__ void write_scores(const ScoresParams& p, int64_t token, const RowSums& sums, uint64_t list, int lane) {
   const bool none = sums.l == 0.f;   // (every word at -inf; NaN is not)
-  const float log_l = __builtin_amdgcn_logf(sums.l), lse = none ? -INFINITY : (sums.m + log_l) * kLn2;
+  const float log_l = __builtin_amdgcn_logf(sums.l), ln_l = log_l * kLn2;
   if (lane == 0) {
-    if (p.lse) p.lse[token] = lse;
+    if (p.lse) p.lse[token] = none ? -INFINITY : fmaf(sums.m, p.scale, ln_l);
     if (p.entropy) p.entropy[token] = none ? 0.f : (log_l - sums.w / sums.l) * kLn2;
     if (p.logp) {
       const int64_t y = p.y[token];
       RowVectors<F32> row;
       row.init(p, token);
-      p.logp[token] = y < 0 || y >= p.vocab ? 0.f : none ? -INFINITY : row.element((int32_t)y) * p.scale - lse;
+      p.logp[token] = y < 0 || y >= p.vocab ? 0.f : none ? -INFINITY : (row.element((int32_t)y) - sums.m) * p.scale - ln_l;
     }
   }
   if (lane < p.n_top) {
     const int64_t to = token * p.n_top + lane;
     if (p.top_ids) p.top_ids[to] = list == 0 ? 0 : (int64_t)(int32_t)~(uint32_t)list;   // (fewer words than n_top: the others are NaN)
-    if (p.top_logp) p.top_logp[to] = none ? -INFINITY : number_of(list) * p.scale - lse;
+    if (p.top_logp) p.top_logp[to] = none ? -INFINITY : (number_of(list) - sums.m) * p.scale - ln_l;
   }
 }
 
@@ -388,9 +392,10 @@ __global__ __launch_bounds__(64 * (W == 1 ? 4 : W)) void scores_kernel(ScoresPar
   RowSums sums;
   LaneBest top;
   uint64_t list = 0;
-  scan_row<F32, TOP>(row, v0, v1, p.scale * kLog2e, lane, sums, top);
-  if constexpr (TOP) list = likeliest<F32, W>(row, v0, v1, top, p.n_top, sums, sums_lds, lists, found[W == 1 ? wave : 0], &count, wave, lane);
-  else if constexpr (W > 1) join_waves<W, false>(sums, list, sums_lds, lists, wave, lane);
+  const float to_log2 = exponents_of(p.scale);
+  scan_row<F32, TOP>(row, v0, v1, to_log2, lane, sums, top);
+  if constexpr (TOP) list = likeliest<F32, W>(row, v0, v1, top, p.n_top, sums, to_log2, sums_lds, lists, found[W == 1 ? wave : 0], &count, wave, lane);
+  else if constexpr (W > 1) join_waves<W, false>(sums, list, to_log2, sums_lds, lists, wave, lane);
   if (W > 1 && wave != 0) return;
   if (segments == 1) {
     write_scores<F32>(p, token, sums, list, lane);
@@ -414,7 +419,7 @@ __global__ __launch_bounds__(64 * kMostSegments) void scores_join_kernel(ScoresP
     sums = ((const Partial*)p.workspace)[at].sums;
     if (TOP && lane < p.n_top) list = ((const uint64_t*)((const Partial*)p.workspace + p.n_tokens * segments))[at * p.n_top + lane];
   }
-  join_waves<kMostSegments, TOP>(sums, list, sums_lds, lists, wave, lane);
+  join_waves<kMostSegments, TOP>(sums, list, exponents_of(p.scale), sums_lds, lists, wave, lane);
   if (wave == 0) write_scores<F32>(p, token, sums, list, lane);
 }
 
@@ -460,16 +465,37 @@ hipError_t launch(const ScoresParams& p, hipStream_t stream) {
 // Every logit is read once and every gradient written once but for the few words that are named: their logits are read before anything is written (the
 // gradient may take the logits' place), and their gradients written once more, whole, behind the others of their part of the row.
 // Bound by memory: 4096 x 32000 fp32 205 us, 1.05 GB at 5.1 TB/s.  (Four runs of a thread loaded before the first is stored: 50 us more in fp32, nothing in bf16.)
+//   A log probability is x scale - lse, off by lse's rounding, 2^-25 of it.  Where |lse| is beyond kFarLse (rows at large finite numbers: a lse of -1e10 is the same for one word and for
+// 128256) that says too little or nothing, and the maximum and the sum are formed again from the row, by the threads of its first part, which then do the others' work too: nobody else
+// reads a row that may be written in its place.  (4096 x 128256 bf16: 346 us, 374 with 16 such rows; 4096 x 32000 fp32: 227 us, 254 with 256, 828 with nothing else.)
+constexpr float kFarLse = 4096.f;
+
 struct RowSlope {
-  float lse, entropy, g_all, g_entropy, scale;
-  bool none;   // a row all at -inf
+  float m, lse, entropy, g_all, g_entropy, scale;   // log p = scale (x - m) - lse
+  bool none;   // a row all at -inf, or to be left out (it may hold anything)
   __device__ __forceinline__ float of_sum(float x) const {   // of the part without named words
-    const float logp = fmaf(x, scale, -lse), p = none ? 0.f : __builtin_amdgcn_exp2f(logp * kLog2e);
-    return p * fmaf(-g_entropy, fmaxf(logp, kNothing) + entropy, g_all);
+    const float logp = fmaf(x - m, scale, -lse), p = __builtin_amdgcn_exp2f(logp * kLog2e);
+    return none ? 0.f : p * fmaf(-g_entropy, fmaxf(logp, kNothing) + entropy, g_all);
   }
 };
 
 constexpr int kSlopeChunk = 8192;   // elements of a part of a row
+
+// A value of each of a part's threads joined over all of them, in all of them.  lds: a number for each wave.
+template <int T, class Join>
+__device__ __forceinline__ float over_part(float x, Join join, float* lds) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) x = join(x, __shfl_xor(x, s, 64));
+  if constexpr (T > 64) {
+    __syncthreads();
+    lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+#pragma unroll
+    for (int i = 1; i < T / 64; ++i) x = join(x, lds[i]);
+  }
+  return x;
+}
 
 // T: threads of a part, of which a work-group of 256 has one or four.
 template <bool F32, bool TO_F32, bool NT, int T>
@@ -481,12 +507,16 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
   const int64_t from = token * p.ld, to = token * p.ld_out;
   // Runs of 8 start at multiples of 8 of the logits' memory; of the gradient's too if its rows lie alike.
   const int32_t before = (int32_t)(from & 7), e_first = chunk * kSlopeChunk - before;
+  __shared__ float joined_lds[T / 64];
   const bool alike = ((from ^ to) & 7) == 0;
   const int64_t y = p.y ? p.y[token] : -1;
   const bool has_y = y >= 0 && y < p.vocab && p.g_logp;
   RowSlope s;
+  s.m = 0.f;
   s.lse = p.lse[token];
   s.none = s.lse == -INFINITY;
+  const bool far = fabsf(s.lse) > kFarLse && !s.none;   // (the same for all threads of a part)
+  if (far && chunk != 0) return;                        // (T = 256: of the whole work-group)
   s.entropy = p.g_entropy ? p.entropy[token] : 0.f;
   s.g_entropy = p.g_entropy ? p.g_entropy[token] : 0.f;
   s.scale = p.scale;
@@ -505,12 +535,33 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
     else ((__bf16*)out)[i] = (__bf16)x;
   };
 
+  if (far) {
+    RowVectors<F32> again;
+    again.init(p.logits, from, vocab);
+    const int32_t vectors = again.vectors();
+    const float to_log2 = exponents_of(p.scale);
+    float m = -INFINITY, l = 0.f;
+    for (int32_t j = tid; j < vectors; j += T) {
+      const u32x4 x = again.load(j);
+#pragma unroll
+      for (int i = 0; i < RowVectors<F32>::VEC; ++i) m = fmaxf(m, RowVectors<F32>::value(x, i));
+    }
+    s.m = over_part<T>(m, [](float a, float b) { return fmaxf(a, b); }, joined_lds);
+    for (int32_t j = tid; j < vectors; j += T) {
+      const u32x4 x = again.load(j);
+#pragma unroll
+      for (int i = 0; i < RowVectors<F32>::VEC; ++i) l += __builtin_amdgcn_exp2f((RowVectors<F32>::value(x, i) - s.m) * to_log2);
+    }
+    s.lse = __builtin_amdgcn_logf(over_part<T>(l, [](float a, float b) { return a + b; }, joined_lds)) * kLn2;
+  }
+  const int32_t e_behind = e_first + (far ? chunks : 1) * kSlopeChunk;
+
   // The words that this thread has to write by itself, if they lie in this part of the row: the given one (thread 0), one of the likeliest
   int64_t named[2] = {tid == 0 && has_y ? y : -1, tid < n_top ? top_id(tid) : -1};
   float named_slope[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if (!is_word(named[i]) || named[i] < e_first || named[i] >= e_first + kSlopeChunk) named[i] = -1;
+    if (!is_word(named[i]) || named[i] < e_first || named[i] >= e_behind) named[i] = -1;
     if (named[i] < 0) continue;
     float g = has_y && named[i] == y ? g_logp : 0.f;
     for (int k = 0; k < n_top; ++k) g += top_id(k) == named[i] ? p.g_top[token * p.n_top + k] : 0.f;
@@ -518,36 +569,39 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
   }
   __syncthreads();
 
+#pragma clang loop unroll(disable)
+  for (int32_t e_part = e_first; e_part < e_behind; e_part += kSlopeChunk) {
 #pragma unroll 4
-  for (int r = 0; r < kSlopeChunk / (8 * T); ++r) {
-    const int32_t e0 = e_first + (tid + T * r) * 8;
-    if (e0 >= vocab) break;
-    if (alike && e0 >= 0 && e0 + 8 <= vocab) {
-      float x[8];
-      if constexpr (F32) {
-        const f32x4 a = load_as<f32x4, NT>(row + 4 * (int64_t)e0), b = load_as<f32x4, NT>(row + 4 * (int64_t)e0 + 16);
+    for (int r = 0; r < kSlopeChunk / (8 * T); ++r) {
+      const int32_t e0 = e_part + (tid + T * r) * 8;
+      if (e0 >= vocab) break;
+      if (alike && e0 >= 0 && e0 + 8 <= vocab) {
+        float x[8];
+        if constexpr (F32) {
+          const f32x4 a = load_as<f32x4, NT>(row + 4 * (int64_t)e0), b = load_as<f32x4, NT>(row + 4 * (int64_t)e0 + 16);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < 4 ? a[i & 3] : b[i & 3];
+          for (int i = 0; i < 8; ++i) x[i] = i < 4 ? a[i & 3] : b[i & 3];
+        } else {
+          const u32x4 a = load_as<u32x4, NT>(row + 2 * (int64_t)e0);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = RowVectors<false>::value(a, i);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = s.of_sum(x[i]) * p.scale;
+        if constexpr (TO_F32) {
+          store_as<NT>(f32x4{x[0], x[1], x[2], x[3]}, out + 4 * (int64_t)e0);
+          store_as<NT>(f32x4{x[4], x[5], x[6], x[7]}, out + 4 * (int64_t)e0 + 16);
+        } else {
+          bf16x8 z;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[i] = (__bf16)x[i];
+          store_as<NT>(z, out + 2 * (int64_t)e0);
+        }
       } else {
-        const u32x4 a = load_as<u32x4, NT>(row + 2 * (int64_t)e0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = RowVectors<false>::value(a, i);
+        for (int i = 0; i < 8; ++i)
+          if (e0 + i >= 0 && e0 + i < vocab) put(e0 + i, s.of_sum(element(e0 + i)) * p.scale);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = s.of_sum(x[i]) * p.scale;
-      if constexpr (TO_F32) {
-        store_as<NT>(f32x4{x[0], x[1], x[2], x[3]}, out + 4 * (int64_t)e0);
-        store_as<NT>(f32x4{x[4], x[5], x[6], x[7]}, out + 4 * (int64_t)e0 + 16);
-      } else {
-        bf16x8 z;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = (__bf16)x[i];
-        store_as<NT>(z, out + 2 * (int64_t)e0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (e0 + i >= 0 && e0 + i < vocab) put(e0 + i, s.of_sum(element(e0 + i)) * p.scale);
     }
   }
   __syncthreads();
