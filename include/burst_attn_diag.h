@@ -89,6 +89,9 @@ int burst_attn_tree_plan(const burst_shape_t* shape, int32_t out[3]);
 /* How a burst_lm_head_scores is dealt: out[0] waves of a work-group that take a row's part together, out[1] such parts of a row.  Host only. */
 int burst_lm_head_scores_plan(const burst_scores_shape_t* shape, int32_t out[2]);
 
+/* out[0] = tokens that a launch of burst_lm_head_scores_bwd takes at most; more go to several.  Host only. */
+int burst_lm_head_scores_bwd_plan(const burst_scores_shape_t* shape, int64_t out[1]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -169,6 +169,8 @@ _lib.burst_lm_head_scores_workspace_bytes.restype = C.c_int64
 _lib.burst_lm_head_scores_workspace_bytes.argtypes = [_P(burst_scores_shape_t)]
 _lib.burst_lm_head_scores_plan.restype = C.c_int
 _lib.burst_lm_head_scores_plan.argtypes = [_P(burst_scores_shape_t), _P(C.c_int32)]
+_lib.burst_lm_head_scores_bwd_plan.restype = C.c_int
+_lib.burst_lm_head_scores_bwd_plan.argtypes = [_P(burst_scores_shape_t), _P(C.c_int64)]
 _lib.burst_lm_head_scores.restype = C.c_int
 _lib.burst_lm_head_scores.argtypes = [_P(burst_scores_shape_t), C.c_void_p, C.c_int32, C.c_int64] + [C.c_void_p] * 7 + [C.c_int64, C.c_void_p]
 _lib.burst_lm_head_scores_bwd.restype = C.c_int
@@ -188,7 +190,7 @@ EXPORTS = ["burst_attn_step_fwd", "burst_attn_steps_fwd", "burst_attn_steps_bwd"
            "burst_lm_head_static_scratch_bytes", "burst_lm_head_tile_plan", "burst_lm_head_loss_noalloc",
            "burst_attn_rope", "burst_attn_cache_append", "burst_attn_decode_workspace_bytes", "burst_attn_decode", "burst_attn_decode_plan",
            "burst_attn_tree_workspace_bytes", "burst_attn_tree", "burst_attn_tree_plan", "burst_attn_cache_copy_pages", "burst_attn_cache_keep_rows",
-           "burst_lm_head_scores_workspace_bytes", "burst_lm_head_scores", "burst_lm_head_scores_bwd", "burst_lm_head_scores_plan"]
+           "burst_lm_head_scores_workspace_bytes", "burst_lm_head_scores", "burst_lm_head_scores_bwd", "burst_lm_head_scores_plan", "burst_lm_head_scores_bwd_plan"]
 
 
 class BurstError(RuntimeError):
@@ -762,6 +764,13 @@ def burst_lm_head_scores_plan(shp):
     out = (C.c_int32 * 2)()
     _check(_lib.burst_lm_head_scores_plan(shp, out))
     return out[0], out[1]
+
+
+def burst_lm_head_scores_bwd_plan(shp):
+    """Tokens that a launch of a burst_lm_head_scores_bwd takes at most (diagnostics)."""
+    out = (C.c_int64 * 1)()
+    _check(_lib.burst_lm_head_scores_bwd_plan(shp, out))
+    return out[0]
 
 
 def _logits(t, shp, device, name):

@@ -1194,6 +1194,13 @@ int burst_lm_head_scores_plan(const burst_scores_shape_t* shape, int32_t out[2])
   return BURST_OK;
 }
 
+int burst_lm_head_scores_bwd_plan(const burst_scores_shape_t* shape, int64_t out[1]) {
+  BURST_TRY(check_scores_shape(shape));
+  if (!out) return BURST_ERR_INVALID_ARG;
+  out[0] = scores_bwd_tokens((int32_t)shape->vocab);
+  return BURST_OK;
+}
+
 int burst_lm_head_scores(const burst_scores_shape_t* shape, const void* logits, int32_t logits_dtype, int64_t ld, const int64_t* y, float* logp, float* lse,
                          float* entropy, float* top_logp, int64_t* top_ids, void* workspace, int64_t workspace_bytes, void* hip_stream) {
   BURST_TRY(check_scores_shape(shape));

@@ -365,6 +365,7 @@ hipError_t launch_scores(const ScoresParams& p, hipStream_t stream);
 hipError_t launch_scores_bwd(const ScoresBwdParams& p, hipStream_t stream);
 int64_t scores_workspace_bytes(int64_t n_tokens, int32_t vocab, int32_t n_top);
 void scores_plan(int64_t n_tokens, int32_t vocab, int32_t out[2]);   // burst_lm_head_scores_plan
+int64_t scores_bwd_tokens(int32_t vocab);                            // burst_lm_head_scores_bwd_plan
 
 // n steps of the query chunk that `p` describes (its own step array is not read).  More than one only without o_part.
 // With a log nothing is launched: it gets the kernel (BURST_KERNEL_ bits) of each launch of step kernels that there would be.

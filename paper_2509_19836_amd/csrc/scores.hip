@@ -614,11 +614,14 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
 // 400 tokens (102 MB) 35.4 / 39.7 us, 600 (154 MB) 52.1 / 50.2, 1200 99.9 / 82.9, 2400 195 / 178, 4096 312 / 296; 8192 in bf16 302 / 258.
 constexpr int64_t kLargeBytes = 128 << 20;
 
+int32_t parts_of_row(int32_t vocab) { return (int32_t)(((int64_t)vocab + 7 + kSlopeChunk - 1) / kSlopeChunk); }
+// A launch has fewer than 2^32 threads; more tokens go to several, in multiples of 8: each begins at a multiple of 16 bytes then, whatever the rows' pitch.
+int64_t tokens_of_launch(int32_t vocab) { return ((int64_t)1 << 23) / parts_of_row(vocab) / 8 * 8; }   // (at most 2^17 + 1 parts)
+
 template <bool F32, bool TO_F32>
 hipError_t launch_bwd(const ScoresBwdParams& p, hipStream_t stream) {
-  const int32_t chunks = (int32_t)(((int64_t)p.vocab + 7 + kSlopeChunk - 1) / kSlopeChunk);
-  // A launch has fewer than 2^32 threads; more tokens go to several.
-  const int64_t each = std::max<int64_t>(1, ((int64_t)1 << 23) / chunks);
+  const int32_t chunks = parts_of_row(p.vocab);
+  const int64_t each = tokens_of_launch(p.vocab);
   // A wave for a row of few words (scores and gradient in us, bf16, a wave / four: 6107 x 357 16.3 / 24.6, 10211 x 1800 29.9 / 34.6, 10211 x 4154 67.7 / 75.4; in fp32 10211 x
   // 8000 228 / 208, 300 x 8000 18.6 / 15.3)
   const bool few = p.vocab <= 4608;
@@ -655,6 +658,8 @@ void scores_plan(int64_t n_tokens, int32_t vocab, int32_t out[2]) {
   out[0] = s.waves;
   out[1] = s.segments;
 }
+
+int64_t scores_bwd_tokens(int32_t vocab) { return tokens_of_launch(vocab); }
 
 hipError_t launch_scores(const ScoresParams& p, hipStream_t stream) {
   if (p.n_tokens == 0) return hipSuccess;
