@@ -649,6 +649,8 @@ def tree(seen=None, first_row=None, tokens=None, sink_rows=0, elsewhere=False):
     A plan that a program keeps; it holds the tensors, whose contents are read when a call that uses it runs."""
     device = torch.cuda.current_device()
     _check_device(device, seen, first_row, tokens)
+    if not 0 <= sink_rows < 1 << 31:
+        raise ValueError(f"sink_rows: a number of 0 to 2^31 - 1 rows expected, not {sink_rows}")
     t = burst_tree_t(None, 0, None, 0, None, sink_rows, int(elsewhere))
     sizes = [None, None]                # batch, sq: of the tensors that there are
     for name, x, dtype in (("seen", seen, torch.int64), ("first_row", first_row, torch.int32), ("tokens", tokens, torch.int32)):

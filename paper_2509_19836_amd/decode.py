@@ -151,13 +151,13 @@ class Draft:
             seen.append([w - (1 << 64) if w >> 63 else w for w in words] + [0] * (sq - len(p)))
             depth.append(deep + [0] * (sq - len(p)))
         places = [[n + i for i in deep] for n, deep in zip(older, depth, strict=True)]
-        cache.grow(self.counts)
         device = cache.rows.device
         first = None if window is None else torch.tensor([[max(0, t - window + 1) for t in row] for row in places], dtype=torch.int32).to(device)
         self.positions = torch.tensor([places], dtype=torch.int32).to(device)
         self.new_rows = torch.tensor(self.counts, dtype=torch.int32).to(device)
         self.tree = lib.tree(torch.tensor(seen, dtype=torch.int64).to(device), first, self.new_rows, sink_rows=0 if window is None else sink_rows)
         self.elsewhere = lib.tree(tokens=self.new_rows, elsewhere=True)
+        cache.grow(self.counts)   # (last: a draft that is refused leaves the cache as it was)
 
     def agreed(self, words, likeliest):
         """The path of each sequence through its draft where every token is the likeliest word after the one before: token 0, which is given, then of the
