@@ -3,7 +3,7 @@
 // Both move bytes and nothing else: 16 of them a thread and access, as many accesses under way as a thread has registers for, and neighbouring
 // threads side by side in the order in which a page lies in memory.
 //   Measured: 64 pages of 64 rows, 32 layers, 8 heads (537 MB read, as many written) 212 us, 5.07 TB/s, what a large copy reaches; with 32 sequences' up to 16 rows in 32 layers
-// a keep takes 5.9 us on the GPU and 6.5 with the host's issue, the copy of three pages in two layers 4.3 and 5.
+// a keep takes 6.6 to 6.9 us, which the host's issue of a call from Python just hides; the copy of three pages in two layers 4.5 to 4.8, and 5.8 a call.
 #include <algorithm>
 
 #include "cache.hpp"

@@ -10,8 +10,8 @@
 // is sorted.  An entry is the number, as a whole one of the same order, over the complement of its index: equal numbers go by the lowest index, rows of equal
 // numbers (masked ones) give a bound that few words reach like any other, and any way of dealing the elements out gives the same words.
 //   A row is a wave's where there are many, else several waves' or several work-groups', whose sums and lists are joined.
-//   Measured: 4001 x 128256 bf16, 20 words 226 us (4.5 TB/s, vector unit 78 % busy; without words 182, 5.6 TB/s); 4096 x 32000 fp32 without words 95 us (5.5 TB/s); 60 x 32000, 8 words 12 us,
-// of which the words are 4.5.  Lists that are kept in order while a row is read took 318 us in the first case.
+//   Measured: 4001 x 128256 bf16, 20 words 226 us (4.5 TB/s, vector unit 88 % busy; without words 182, 5.6 TB/s); 4096 x 32000 fp32 without words 98 us (5.4 TB/s); 60 x 32000, 8 words
+// 12.5 us, of which the words are 4.5.  Lists that are kept in order while a row is read took 318 us in the first case.
 #include <algorithm>
 #include <type_traits>
 
@@ -425,18 +425,19 @@ __global__ __launch_bounds__(64 * kMostSegments) void scores_join_kernel(ScoresP
 
 // How a row is dealt out: waves of a work-group, and work-groups.  us with 8 (20 where there are 300 tokens or more) words, bf16:
 //   tokens x vocabulary          1 wave     4     16     16 x 4 work-groups and a join
-//   1 x 32000                        -   10.7   12.5   16.0
-//   1 x 128256                       -   21.6   18.1   16.5
-//   1 x 262144                       -   35.6   25.4   17.7 (x 8: 16.6)
-//   60 x 5000                     10.9    8.6   12.3
-//   60 x 32000                    29.4   12.0   13.3   16.5
-//   60 x 65000                       -   16.8   15.6   17.2
-//   60 x 262144                      -   41.9   27.1   20.4 (x 8, which is more work-groups than compute units: 28.6)
-//   300 x 32000                   39.4   17.1   25.4
-//   800 x 128256                   149   65.3   83.5
-//   16000 x 5000                  73.8    144    657
-//   4001 x 32000                  81.7   83.6    188
-//   4001 x 128256                  269    227    328
+//   1 x 32000                     24.2   11.2   13.3   16.8
+//   1 x 128256                    62.2   23.0   19.3   17.4
+//   1 x 262144                     120   38.3   26.6   18.1 (x 8: 16.5)
+//   60 x 5000                     11.1    8.7   13.0
+//   60 x 32000                    29.5   12.4   14.2   17.3
+//   60 x 65000                    57.7   17.2   16.4   17.9
+//   60 x 262144                    224   44.4   28.4   20.8 (x 8, which is more work-groups than compute units: 29.0)
+//   300 x 32000                   39.3   17.0   26.4
+//   800 x 128256                   149   65.7   84.2
+//   16000 x 5000                  70.4    146    704
+//   4001 x 32000                  80.1   75.9    198
+//   4001 x 128256                  265    225    329
+// Calls without words go by the same rule, which was not measured for them.
 // (A launch has fewer than 2^32 threads, so the most tokens get a wave each, four of them a work-group.)
 struct ScoresShape {
   int waves, segments;
@@ -464,7 +465,7 @@ hipError_t launch(const ScoresParams& p, hipStream_t stream) {
 // d x_j = scale * [ p_j (g_lse - g_logp - sum g_top - g_entropy (log p_j + entropy)) + g_logp [j = y] + sum over k of g_top,k [j = id_k] ]
 // Every logit is read once and every gradient written once but for the few words that are named: their logits are read before anything is written (the
 // gradient may take the logits' place), and their gradients written once more, whole, behind the others of their part of the row.
-// Bound by memory: 4096 x 32000 fp32 205 us, 1.05 GB at 5.1 TB/s.  (Four runs of a thread loaded before the first is stored: 50 us more in fp32, nothing in bf16.)
+// Bound by memory: 4096 x 32000 fp32 202 us, 1.05 GB at 5.2 TB/s.  (Four runs of a thread loaded before the first is stored: 50 us more in fp32, nothing in bf16.)
 //   A log probability is x scale - lse, off by lse's rounding, 2^-25 of it.  Where |lse| is beyond kFarLse (rows at large finite numbers: a lse of -1e10 is the same for one word and for
 // 128256) that says too little or nothing, and the maximum and the sum are formed again from the row, by the threads of its first part, which then do the others' work too: nobody else
 // reads a row that may be written in its place.  (4096 x 128256 bf16: 346 us, 374 with 16 such rows; 4096 x 32000 fp32: 227 us, 254 with 256, 828 with nothing else.)
@@ -611,7 +612,7 @@ __global__ __launch_bounds__(256) void scores_bwd_kernel(ScoresBwdParams p, int3
 }
 
 // Logits and gradients of more bytes than this are read and written without keeping their lines.  Of 32000 words in fp32, scores and gradient, kept / not:
-// 400 tokens (102 MB) 35.4 / 39.7 us, 600 (154 MB) 52.1 / 50.2, 1200 99.9 / 82.9, 2400 195 / 178, 4096 312 / 296; 8192 in bf16 302 / 258.
+// 400 tokens (102 MB) 35.3 / 39.6 us, 600 (154 MB) 52.4 / 49.8, 1200 101 / 82.7, 2400 196 / 179, 4096 312 / 296; 8192 in bf16 294 / 258.
 constexpr int64_t kLargeBytes = 128 << 20;
 
 int32_t parts_of_row(int32_t vocab) { return (int32_t)(((int64_t)vocab + 7 + kSlopeChunk - 1) / kSlopeChunk); }
@@ -622,8 +623,8 @@ template <bool F32, bool TO_F32>
 hipError_t launch_bwd(const ScoresBwdParams& p, hipStream_t stream) {
   const int32_t chunks = parts_of_row(p.vocab);
   const int64_t each = tokens_of_launch(p.vocab);
-  // A wave for a row of few words (scores and gradient in us, bf16, a wave / four: 6107 x 357 16.3 / 24.6, 10211 x 1800 29.9 / 34.6, 10211 x 4154 67.7 / 75.4; in fp32 10211 x
-  // 8000 228 / 208, 300 x 8000 18.6 / 15.3)
+  // A wave for a row of few words (scores and gradient in us, bf16, a wave / four: 6107 x 357 16.4 / 24.3, 10211 x 1800 28.7 / 33.2, 10211 x 4154 68.6 / 77.0; in fp32 10211 x
+  // 8000 219 / 177, 300 x 8000 20.0 / 15.0)
   const bool few = p.vocab <= 4608;
   const bool large = p.n_tokens * p.vocab * ((F32 ? 4 : 2) + (TO_F32 ? 4 : 2)) > kLargeBytes;
   for (int64_t first = 0; first < p.n_tokens; first += each) {

@@ -16,9 +16,10 @@
 // first rows and its own.  The units are dealt evenly to shares, a work-group each for every key head and block of columns; a piece that is
 // a whole sequence is written out, others go to the workspace and tree_join_kernel adds them up in a fixed order.
 //
-// Measured, with the join: 4 sequences of 32768 rows, 64 tokens, 64 query heads over 8 (512 columns, bf16) 396-404 us, three products executed for two at 1030 TFLOP/s.  Scalar work on
-// masks and pages is kept out of the tiles (looked up tile by tile it took 8 % more).  Two teams of waves that take products and exponentials in turn, as in a step of the ring, gave nothing here (each
-// team brings tiles of its own), nor did 256 columns a work-group.  16 sequences of up to 4096 rows, 12 tokens, 32 over 8 heads: 25 us and a join of 6.5; 32 of up to 49152, a
+// Measured, with the join: 4 sequences of 32768 rows, 64 tokens, 64 query heads over 8 (512 columns, bf16) 391-404 us, three products executed for two at 1020-1050 TFLOP/s, matrix pipe 50 % busy,
+// vector unit 53 %.  Scalar work on
+// masks and pages is kept out of the tiles (looked up tile by tile it took 8 % more).  Two teams of waves that take products and exponentials in turn gave nothing where each team brought tiles of its
+// own, nor did 256 columns a work-group (both with P in one part); teams over one set of tiles, as in a step of the ring, were not tried.  16 sequences of up to 4096 rows, 12 tokens, 32 over 8 heads: 25 us and a join of 6.5; 32 of up to 49152, a
 // window of 16384, 8 tokens, 64 over 8 heads, e4m3 165 us, 4.7 TB/s.
 #include "tree.hpp"
 
@@ -262,10 +263,12 @@ TreeShape tree_shape(int32_t batch, int32_t sq, int32_t q_heads, int32_t kv_head
   const int64_t per_seq = (int64_t)kv_heads * s.blocks, unit = s.columns <= 32 ? 128 : 64, max_units = std::max<int64_t>(1, (max_rows + unit - 1) / unit);
   // A work-group for a whole sequence where they fill the chip, or where its tiles take less time than dealing them out, a second launch and the join of pieces: the
   // more sequences there are, the longer those take.  us, whole / dealt, bf16, head_dim 128:
-  //   80 columns   32 work-groups: 256 rows 13.1 / 16.8, 512 19.2 / 18.8;   64: 512 19.6 / 22.7, 1024 30.9 / 25.4;   128: 512 20.1 / 25.6, 1024 31.4 / 31.8;
-  //                240: 1024 37.7 / 46.6, 2048 61.6 / 71.4, 4096 109 / 113, of up to 1024 rows 31.4 / 29.5, of up to 4096 101 / 44.9
+  //   80 columns   32 work-groups: 256 rows 14.6 / 15.1, 512 21.8 / 17.7;   64: 512 22.6 / 22.4, 1024 37.1 / 25.8;   128: 512 23.1 / 25.5, 1024 37.5 / 31.2;
+  //                240: 1024 40.5 / 46.0, 2048 69.5 / 69.9, 4096 128 / 113, of up to 1024 rows 37.3 / 30.3, of up to 4096 125 / 47.1
   //   16 columns   64 work-groups: 512 rows 10.6 / 14.2, 1024 13.4 / 18.5, 4096 47.8 / 32.0;   240: 1024 29.3 / 31.7, of up to 1024 15.5 / 22.9, of up to 4096 50.5 / 35.8
   //   16 columns   2 work-groups: 1024 rows 12.5 / 12.5;   32 columns, e4m3: 16.2 / 14.3;   16 columns, head_dim 64: 2040 rows 15.0 / 12.0, 12 work-groups of 777 10.4 / 11.0
+  // From kTreeFit work-groups on every sequence is whole.  That costs nothing where they are alike, and time where they are not: 512 work-groups, 80 columns, 1024 rows 61.6 / 61.4, 4096 206 / 205,
+  // of up to 4096 rows 130 / 83.5;   40 columns, of up to 7487 rows 187 / 125;   16 columns, 1024 rows 51.8 / 47.7, of up to 1024 27.7 / 30.7, of up to 4096 91 / 64.5.
   const int64_t groups = batch * per_seq, whole = s.columns <= 32 ? s.columns == 16 || groups >= 64 ? 1024 : 768 : std::max({(int64_t)256, std::min((int64_t)512, 8 * groups), 4 * groups});
   s.direct = groups >= kTreeFit || max_rows <= whole;
   s.shares = (int32_t)(s.direct ? batch : std::min<int64_t>(batch * max_units, std::max<int64_t>(1, kTreeFit / per_seq)));

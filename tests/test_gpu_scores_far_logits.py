@@ -63,7 +63,7 @@ def spread(x, scale):
 
 
 def near(a, b, tol, what):
-    b = np.where(np.abs(b) > LARGEST, np.sign(b) * np.inf, b)
+    b = np.where(np.abs(b) > LARGEST, np.copysign(np.inf, b), b)
     with np.errstate(invalid="ignore"):
         same = (a == b) | (np.abs(a - b) <= tol)
     assert same.all(), (what, np.argwhere(~same)[:5].tolist(), a[~same][:5], b[~same][:5])
